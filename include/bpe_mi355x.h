@@ -491,10 +491,135 @@ int bpe_decode(const bpe_vocab *vocab, const int32_t *ids, int64_t n_tokens,
                int64_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------- */
+/* From a model's hidden states to the next ids, in the numbering of a        */
+/* vocabulary: logits (bpe_linear), the tokens that a grammar lets follow      */
+/* (bpe_grammar_masks), penalties, biases and masks on logits                  */
+/* (bpe_adjust_logits), the best tokens (bpe_top_tokens), the grammar's states */
+/* behind the chosen ones (bpe_grammar_advance); bpe_decode turns those into   */
+/* text.  Every call only enqueues kernels on `stream`: no allocation, no      */
+/* synchronisation, no host-device copy; all may be captured into a graph.     */
+/* Matrices are row-major, `stride` = elements from a row to the next, at      */
+/* least the row's length (of one row any); pointers are aligned to their type */
+/* and need no more.  Outputs must not overlap inputs unless a call says so.   */
+typedef enum { BPE_F32 = 0, BPE_BF16 = 1, BPE_F16 = 2 } bpe_dtype_t;
+
+typedef enum {
+    BPE_ACT_NONE = 0,
+    BPE_ACT_RELU = 1,           /* max(v, 0)                                              */
+    BPE_ACT_GELU = 2,           /* v / 2 * (1 + erf(v / sqrt 2))                          */
+    BPE_ACT_GELU_TANH = 3,      /* v / 2 * (1 + tanh(sqrt(2 / pi) * (v + 0.044715 v^3)))  */
+    BPE_ACT_SILU = 4            /* v / (1 + exp(-v))                                      */
+} bpe_activation_t;
+
+/* Device bytes that bpe_linear needs for these sizes, 0 for many (pure function). */
+int64_t bpe_linear_workspace_bytes(int64_t m, int64_t n, int64_t k);
+
+/*
+ * out[i][j] = activation(sum over t of x[i][t] * weight[j][t] + bias[j]) + residual[i][j]
+ *   x          device [m][k], weight: device [n][k], both of `dtype` (BPE_BF16 or BPE_F16)
+ *   bias       device [n] of bias_dtype (any) or NULL
+ *   residual   device [m][n] of out_dtype or NULL; may be `out` itself with the same stride
+ *   out        device [m][n] of out_dtype (BPE_F32 or `dtype`)
+ *   workspace  device, 256-byte aligned, >= bpe_linear_workspace_bytes(m, n, k); may be NULL if that is 0.
+ *              Need not be initialised; calls that share one must be ordered on one stream
+ * Products and sums in 32 bits, rounded once to out_dtype.  m, n, k >= 0, each below 2^30 (with k == 0 the sum is 0);
+ * matrices may have more than 2^32 elements.  The order of the sum goes by the sizes and the alignment alone.
+ */
+int bpe_linear(const void *x, int64_t x_stride, const void *weight, int64_t weight_stride, int dtype,
+               int64_t m, int64_t n, int64_t k, const void *bias, int bias_dtype, const void *residual,
+               int64_t residual_stride, int activation, void *out, int64_t out_stride, int out_dtype,
+               void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * A grammar: a deterministic automaton over bytes.  transitions: host int32 [n_states][256], the state behind each byte,
+ * or a negative value where the byte ends the walk (BPE_ERR_ID_RANGE for values from n_states on); accepting: host uint8
+ * [n_states], != 0 where the answer may end, or NULL for nowhere; 1 <= n_states < 65535.  One device allocation, owned by
+ * the handle (bytes that no state tells apart share a column: 2 bytes per state and class of bytes).
+ */
+typedef struct bpe_grammar bpe_grammar;
+typedef struct {
+    int64_t n_states;
+    int64_t device_bytes;
+    int32_t n_classes;          /* classes of bytes */
+    int32_t reserved;
+} bpe_grammar_info_t;
+int bpe_grammar_build(const int32_t *transitions, const uint8_t *accepting, int64_t n_states, bpe_grammar **out_grammar);
+int bpe_grammar_free(bpe_grammar *grammar);
+int bpe_grammar_info(const bpe_grammar *grammar, bpe_grammar_info_t *info);
+
+/*
+ * Which tokens may come next: bit v % 32 of masks[i][v / 32] is 1 where the bytes of token v lead from states[i] to a
+ * state without ending the walk.  Ids that stand for no token have bit 0, so do the bits behind n_vocab in the last word
+ * of a row; bit end_id is 1 where states[i] is accepting (also if the vocabulary has a token of that id).
+ *   states              device int32 [n]; a row whose state is not one of the grammar's is all 0
+ *   ids_are_output_ids  != 0: bits are numbered by the vocabulary's output ids
+ *   n_vocab             bits per row, at least 1: a model may have more logits than the vocabulary has ids, or fewer
+ *   end_id              in [0, n_vocab), or -1 for none
+ *   masks               device uint32 [n] rows of (n_vocab + 31) / 32 words, mask_stride words apart
+ */
+int bpe_grammar_masks(const bpe_vocab *vocab, const bpe_grammar *grammar, const int32_t *states, int64_t n,
+                      int ids_are_output_ids, int64_t n_vocab, int64_t end_id, uint32_t *masks, int64_t mask_stride,
+                      void *stream);
+
+/*
+ * out_states[i] = the state behind the bytes of token ids[i], from states[i]; -1 where the walk ends, for an id that stands
+ * for no token and from a state that is not one of the grammar's.  ids[i] == end_id (>= 0) stays in an accepting state
+ * and ends the walk in others.  out_states may be states.  All device int32 [n].
+ */
+int bpe_grammar_advance(const bpe_vocab *vocab, const bpe_grammar *grammar, const int32_t *states, const int32_t *ids,
+                        int64_t n, int ids_are_output_ids, int64_t end_id, int32_t *out_states, void *stream);
+
+/* What bpe_adjust_logits does to a row; all pointers are device pointers, any may be NULL (nothing of that kind). */
+typedef struct {
+    const float *repetition;        /* [rows], > 0; NULL = 1 */
+    const float *frequency;         /* [rows]; NULL = 0 */
+    const float *presence;          /* [rows]; NULL = 0 */
+    const int32_t *history;         /* [n_history] the tokens that came before, row by row; ids outside [0, n_vocab) count for nothing */
+    const int32_t *history_offsets; /* [rows + 1]; row r has history[history_offsets[r] .. history_offsets[r + 1]) */
+    int64_t n_history;              /* < 2^31; offsets are clamped to [0, n_history] */
+    const int32_t *bias_ids;        /* [n_bias], row by row; ids outside [0, n_vocab) are skipped; of an id that a row lists more than once the last entry counts */
+    const float *bias_values;       /* [n_bias] */
+    const int32_t *bias_offsets;    /* [rows + 1], clamped to [0, n_bias] */
+    int64_t n_bias;                 /* < 2^31 */
+    const uint32_t *masks;          /* [n_masks] rows as bpe_grammar_masks writes them, mask_stride words apart */
+    int64_t mask_stride;
+    int64_t n_masks;
+    const int32_t *mask_index;      /* [rows]: the row's mask, a negative value for none; one that is too large allows no token.  NULL: row r has mask r (n_masks >= rows) */
+} bpe_logit_rules;
+
+/*
+ * out = logits under the rules: with c = how often token v is in the row's history,
+ *   x = logits[r][v];  if c > 0: x = (x > 0 ? x / repetition : x * repetition) - frequency * c - presence;
+ *   if v is in the row's bias list: x = x + its value;  if the bit of v in the row's mask is 0: x = -infinity
+ * in this order, in 32 bits, each operation rounded by itself, and once more to out_dtype; what a mask takes out is
+ * -infinity whatever the logit was.  A row may be left with nothing but -infinity.
+ *   logits   device [rows][n_vocab] of dtype;  out: of out_dtype (BPE_F32 or dtype); may be `logits` itself if the types and strides
+ *            are equal.  rules may be NULL (a conversion).  rows < 2^31, 1 <= n_vocab < 2^30
+ */
+int bpe_adjust_logits(const void *logits, int64_t logits_stride, int dtype, int64_t rows, int64_t n_vocab,
+                      const bpe_logit_rules *rules, void *out, int64_t out_stride, int out_dtype, void *stream);
+
+/* Device bytes that bpe_top_tokens needs (pure function). */
+int64_t bpe_top_tokens_workspace_bytes(int64_t rows, int64_t n_vocab, int64_t k);
+
+/*
+ * The k best tokens of every row, best first, equal ones by their index.
+ *   logits     device [rows][n_vocab] of dtype;  1 <= k <= min(256, n_vocab); rows < 2^31, n_vocab < 2^30
+ *   ids        device int32 [rows][k], out; -1 where the row has no further token above -infinity
+ *   logprobs   device float [rows][k], out: logit - lse; -infinity where the id is -1
+ *   lse        device float [rows] or NULL, out: log of the sum of exp(logit) over the row, -infinity for a row of nothing else
+ *   workspace  device, 256-byte aligned, >= bpe_top_tokens_workspace_bytes(rows, n_vocab, k); as for bpe_linear
+ * Statistics in 32 bits.  NaN ranks above +infinity, and a row that holds a NaN has NaN for lse and logprobs (as the formula
+ * gives; so has +infinity for its own logprob).
+ */
+int bpe_top_tokens(const void *logits, int64_t logits_stride, int dtype, int64_t rows, int64_t n_vocab, int64_t k,
+                   int32_t *ids, float *logprobs, float *lse, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------- */
 /* Preallocated workspace pool (the paper's profiling, section 5.3, finds     */
 /* allocation to be 70-80 % of its API time and names pooling as the next     */
 /* step).  One allocation at creation, none afterwards.  The buffer is large   */
-/* enough for every entry point that takes a workspace: bpe_encode and        */
+/* enough for every entry point above that encodes or decodes: bpe_encode and  */
 /* bpe_encode_raw on up to max_bytes bytes, max_pieces pieces and max_pieces  */
 /* sequences, bpe_pretokenize on max_bytes bytes, bpe_decode of max_bytes     */
 /* tokens.  Calls that share it must be ordered on one stream.                */

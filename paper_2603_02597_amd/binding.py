@@ -24,6 +24,8 @@ EXPORTS = [
     "bpe_pretokenize_workspace_bytes", "bpe_pretokenize", "bpe_encode_raw_workspace_bytes", "bpe_encode_raw",
     "bpe_encode_raw_timed", "bpe_vocab_build", "bpe_vocab_free", "bpe_vocab_info", "bpe_map_ids",
     "bpe_decode_workspace_bytes", "bpe_decode", "bpe_host_visible", "bpe_batch_in", "bpe_batch_ids_out", "bpe_batch_bytes_out",
+    "bpe_linear_workspace_bytes", "bpe_linear", "bpe_grammar_build", "bpe_grammar_free", "bpe_grammar_info", "bpe_grammar_masks",
+    "bpe_grammar_advance", "bpe_adjust_logits", "bpe_top_tokens_workspace_bytes", "bpe_top_tokens",
 ]
 
 
@@ -43,6 +45,19 @@ class _VocabInfo(ctypes.Structure):
     _fields_ = [("n_ids", ctypes.c_int64), ("n_output_ids", ctypes.c_int64), ("pool_bytes", ctypes.c_int64),
                 ("device_bytes", ctypes.c_int64), ("max_token_bytes", ctypes.c_int32),
                 ("has_output_ids", ctypes.c_int32)]
+
+
+class _GrammarInfo(ctypes.Structure):
+    _fields_ = [("n_states", ctypes.c_int64), ("device_bytes", ctypes.c_int64), ("n_classes", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class _LogitRules(ctypes.Structure):
+    _fields_ = [("repetition", ctypes.c_void_p), ("frequency", ctypes.c_void_p), ("presence", ctypes.c_void_p),
+                ("history", ctypes.c_void_p), ("history_offsets", ctypes.c_void_p), ("n_history", ctypes.c_int64),
+                ("bias_ids", ctypes.c_void_p), ("bias_values", ctypes.c_void_p), ("bias_offsets", ctypes.c_void_p),
+                ("n_bias", ctypes.c_int64), ("masks", ctypes.c_void_p), ("mask_stride", ctypes.c_int64),
+                ("n_masks", ctypes.c_int64), ("mask_index", ctypes.c_void_p)]
 
 
 class _PlanLaunch(ctypes.Structure):
@@ -164,6 +179,26 @@ def load_library():
     lib.bpe_decode_workspace_bytes.argtypes = [i64]
     lib.bpe_decode.restype = i32
     lib.bpe_decode.argtypes = [vp, vp, i64, vp, i32, vp, i64, vp, vp, vp, i64, vp]
+    lib.bpe_linear_workspace_bytes.restype = i64
+    lib.bpe_linear_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.bpe_linear.restype = i32
+    lib.bpe_linear.argtypes = [vp, i64, vp, i64, i32, i64, i64, i64, vp, i32, vp, i64, i32, vp, i64, i32, vp, i64, vp]
+    lib.bpe_grammar_build.restype = i32
+    lib.bpe_grammar_build.argtypes = [vp, vp, i64, ctypes.POINTER(vp)]
+    lib.bpe_grammar_free.restype = i32
+    lib.bpe_grammar_free.argtypes = [vp]
+    lib.bpe_grammar_info.restype = i32
+    lib.bpe_grammar_info.argtypes = [vp, ctypes.POINTER(_GrammarInfo)]
+    lib.bpe_grammar_masks.restype = i32
+    lib.bpe_grammar_masks.argtypes = [vp, vp, vp, i64, i32, i64, i64, vp, i64, vp]
+    lib.bpe_grammar_advance.restype = i32
+    lib.bpe_grammar_advance.argtypes = [vp, vp, vp, vp, i64, i32, i64, vp, vp]
+    lib.bpe_adjust_logits.restype = i32
+    lib.bpe_adjust_logits.argtypes = [vp, i64, i32, i64, i64, ctypes.POINTER(_LogitRules), vp, i64, i32, vp]
+    lib.bpe_top_tokens_workspace_bytes.restype = i64
+    lib.bpe_top_tokens_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.bpe_top_tokens.restype = i32
+    lib.bpe_top_tokens.argtypes = [vp, i64, i32, i64, i64, i64, vp, vp, vp, vp, i64, vp]
     lib.bpe_pool_create.restype = i32
     lib.bpe_pool_create.argtypes = [i64, i64, ctypes.POINTER(vp)]
     lib.bpe_pool_destroy.restype = i32
@@ -193,13 +228,15 @@ def _host_i32(a, shape=None):
 # tensors and a stream took 6 of the 9 us of a 4 KB encode when each looked torch up and compared dtypes by name).
 _torch = None
 _dtypes = {}
+_codes = {}
 _raw_stream = None
 
 
 def _load_torch():
     global _torch, _raw_stream
     import torch
-    _dtypes.update(uint8=torch.uint8, int32=torch.int32)
+    _dtypes.update(uint8=torch.uint8, int32=torch.int32, float32=torch.float32)
+    _codes.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})       # bpe_dtype_t
     get, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
     if get is not None and device is not None:
         _raw_stream = lambda: get(device())       # what torch.cuda.current_stream().cuda_stream reads, without the object
@@ -224,6 +261,21 @@ def _stream_ptr(stream):
     if _torch is None:
         _load_torch()
     return _raw_stream()
+
+
+def _rows(t, what: str):
+    """(pointer, stride, type code) of a matrix on the GPU whose rows are contiguous."""
+    if _torch is None:
+        _load_torch()
+    if not isinstance(t, _torch.Tensor) or not t.is_cuda or t.dim() != 2:
+        raise TypeError(f"{what}: expected a two-dimensional torch tensor on the GPU")
+    code = _codes.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what}: expected float32, bfloat16 or float16, got {t.dtype}")
+    stride, step = t.stride()
+    if step != 1 and t.shape[1] > 1:
+        raise TypeError(f"{what}: the elements of a row must be next to each other")
+    return t.data_ptr(), stride, code
 
 
 def bpe_table_capacity(n_merges: int) -> int:
@@ -505,6 +557,171 @@ def bpe_decode(vocab: Vocab, ids, out_bytes, workspace, token_byte_offsets=None,
         vocab._h, _dev_ptr(ids, "int32"), n, _opt_ptr(n_tokens_device, "int32"), 1 if ids_are_output_ids else 0,
         _dev_ptr(out_bytes, "uint8"), out_bytes.numel(), _opt_ptr(token_byte_offsets, "int32"),
         _opt_ptr(n_bytes, "int32"), _dev_ptr(workspace, "uint8"), workspace.numel(), _stream_ptr(stream)))
+
+
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+def bpe_linear_workspace_bytes(m: int, n: int, k: int) -> int:
+    return _check(load_library().bpe_linear_workspace_bytes(int(m), int(n), int(k)))
+
+
+def bpe_linear(x, weight, out, bias=None, residual=None, activation: str = "none", workspace=None, stream=None):
+    """Enqueue out = activation(x @ weight.T + bias) + residual; x [m, k] and weight [n, k] bfloat16 or float16, out [m, n]
+    float32 or of their type, residual of out's type (it may be out).  Does not synchronise."""
+    px, sx, code = _rows(x, "x")
+    pw, sw, w_code = _rows(weight, "weight")
+    po, so, o_code = _rows(out, "out")
+    m, k = x.shape
+    n = weight.shape[0]
+    if weight.shape[1] != k or out.shape[0] != m or out.shape[1] != n:
+        raise ValueError(f"shapes do not match: x {tuple(x.shape)}, weight {tuple(weight.shape)}, out {tuple(out.shape)}")
+    if w_code != code:
+        raise TypeError("x and weight must have the same dtype")
+    act = ACTIVATIONS.get(activation)
+    if act is None:
+        raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}, got {activation!r}")
+    pb = b_code = pr = sr = 0
+    if bias is not None:
+        if not isinstance(bias, _torch.Tensor) or not bias.is_cuda or not bias.is_contiguous() or bias.numel() != n or bias.dtype not in _codes:
+            raise TypeError(f"bias: expected {n} contiguous elements of float32, bfloat16 or float16 on the GPU")
+        pb, b_code = bias.data_ptr(), _codes[bias.dtype]
+    if residual is not None:
+        pr, sr, r_code = _rows(residual, "residual")
+        if r_code != o_code or residual.shape != out.shape:
+            raise TypeError("residual must have the shape and the dtype of out")
+    _check(load_library().bpe_linear(px, sx, pw, sw, code, m, n, k, pb, b_code, pr, sr, act, po, so, o_code,
+                                     _opt_ptr(workspace, "uint8"), 0 if workspace is None else workspace.numel(), _stream_ptr(stream)))
+
+
+class Grammar:
+    """Device-resident automaton over bytes (owns its device memory): ``transitions`` int [n_states, 256], negative
+    where a byte ends the walk; ``accepting`` [n_states], true where the answer may end."""
+
+    def __init__(self, transitions, accepting=None):
+        lib = load_library()
+        t, tp = _host_i32(transitions, (-1, 256))
+        a = None if accepting is None else np.ascontiguousarray(np.asarray(accepting) != 0, dtype=np.uint8).reshape(-1)
+        if a is not None and a.size != t.shape[0]:
+            raise ValueError(f"accepting has {a.size} entries for {t.shape[0]} states")
+        h = ctypes.c_void_p()
+        _check(lib.bpe_grammar_build(tp, None if a is None else a.ctypes.data_as(ctypes.c_void_p), t.shape[0], ctypes.byref(h)))
+        self._h = h
+        info = _GrammarInfo()
+        _check(lib.bpe_grammar_info(self._h, ctypes.byref(info)))
+        self.info = {f: getattr(info, f) for f in ("n_states", "device_bytes", "n_classes")}
+
+    def free(self):
+        if getattr(self, "_h", None):
+            load_library().bpe_grammar_free(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+def bpe_grammar_build(transitions, accepting=None) -> Grammar:
+    return Grammar(transitions, accepting)
+
+
+def _mask_rows(masks, n_vocab: int):
+    if _torch is None:
+        _load_torch()
+    if not isinstance(masks, _torch.Tensor) or not masks.is_cuda or masks.dim() != 2 or masks.dtype is not _torch.int32:
+        raise TypeError("masks: expected a two-dimensional int32 tensor on the GPU")
+    if masks.shape[1] < (n_vocab + 31) // 32:
+        raise ValueError(f"masks: {n_vocab} bits need {(n_vocab + 31) // 32} words per row, got {masks.shape[1]}")
+    stride, step = masks.stride()
+    if step != 1 and masks.shape[1] > 1:
+        raise TypeError("masks: the words of a row must be next to each other")
+    return masks.data_ptr(), stride
+
+
+def bpe_grammar_masks(vocab: Vocab, grammar: Grammar, states, masks, n_vocab: int | None = None, end_id: int = -1,
+                      ids_are_output_ids: bool = False, stream=None):
+    """Enqueue masks[i] = the tokens that the grammar lets follow in states[i] (int32), one bit each in int32 words;
+    ``n_vocab`` bits per row, as many as the vocabulary has ids unless it is given."""
+    if n_vocab is None:
+        n_vocab = vocab.info["n_output_ids" if ids_are_output_ids else "n_ids"]
+    pm, sm = _mask_rows(masks, n_vocab)
+    n = states.numel()
+    if masks.shape[0] < n:
+        raise ValueError(f"masks has {masks.shape[0]} rows for {n} states")
+    _check(load_library().bpe_grammar_masks(vocab._h, grammar._h, _dev_ptr(states, "int32"), n, 1 if ids_are_output_ids else 0,
+                                            n_vocab, end_id, pm, sm, _stream_ptr(stream)))
+
+
+def bpe_grammar_advance(vocab: Vocab, grammar: Grammar, states, ids, out_states, end_id: int = -1,
+                        ids_are_output_ids: bool = False, stream=None):
+    """Enqueue out_states[i] = the state behind token ids[i] from states[i] (int32; out_states may be states)."""
+    n = states.numel()
+    if ids.numel() != n or out_states.numel() < n:
+        raise ValueError("states, ids and out_states must have the same length")
+    _check(load_library().bpe_grammar_advance(vocab._h, grammar._h, _dev_ptr(states, "int32"), _dev_ptr(ids, "int32"), n,
+                                              1 if ids_are_output_ids else 0, end_id, _dev_ptr(out_states, "int32"), _stream_ptr(stream)))
+
+
+def bpe_adjust_logits(logits, out, history=None, history_offsets=None, repetition=None, frequency=None, presence=None,
+                      bias_ids=None, bias_values=None, bias_offsets=None, masks=None, mask_index=None, stream=None):
+    """Enqueue out = logits [rows, n_vocab] with penalties for the tokens of each row's history, biases and masks (see
+    bpe_logit_rules).  History and biases are lists of all rows with int32 offsets [rows + 1]; repetition, frequency and
+    presence float32 [rows]; masks int32 words as bpe_grammar_masks writes them, mask_index int32 [rows].  out may be logits."""
+    pl, sl, code = _rows(logits, "logits")
+    po, so, o_code = _rows(out, "out")
+    rows, n_vocab = logits.shape
+    if out.shape != logits.shape:
+        raise ValueError("logits and out must have the same shape")
+    r = _LogitRules()
+    if history is not None:
+        r.history, r.history_offsets, r.n_history = _dev_ptr(history, "int32"), _row_list(history_offsets, "int32", rows + 1, "history_offsets"), history.numel()
+        if repetition is not None:
+            r.repetition = _row_list(repetition, "float32", rows, "repetition")
+        if frequency is not None:
+            r.frequency = _row_list(frequency, "float32", rows, "frequency")
+        if presence is not None:
+            r.presence = _row_list(presence, "float32", rows, "presence")
+    elif repetition is not None or frequency is not None or presence is not None:
+        raise ValueError("penalties need a history")
+    if bias_ids is not None:
+        if bias_values is None or bias_values.numel() != bias_ids.numel():
+            raise ValueError("bias_ids and bias_values must have the same length")
+        r.bias_ids, r.bias_values, r.n_bias = _dev_ptr(bias_ids, "int32"), _dev_ptr(bias_values, "float32"), bias_ids.numel()
+        r.bias_offsets = _row_list(bias_offsets, "int32", rows + 1, "bias_offsets")
+    elif bias_values is not None or bias_offsets is not None:
+        raise ValueError("bias_values and bias_offsets need bias_ids")
+    if masks is not None:
+        r.masks, r.mask_stride = _mask_rows(masks, n_vocab)
+        r.n_masks = masks.shape[0]
+        if mask_index is not None:
+            r.mask_index = _row_list(mask_index, "int32", rows, "mask_index")
+    elif mask_index is not None:
+        raise ValueError("mask_index needs masks")
+    _check(load_library().bpe_adjust_logits(pl, sl, code, rows, n_vocab, ctypes.byref(r), po, so, o_code, _stream_ptr(stream)))
+
+
+def _row_list(t, dtype_name: str, n: int, what: str):
+    if t is None or t.numel() != n:
+        raise ValueError(f"{what}: expected {n} elements")
+    return _dev_ptr(t, dtype_name)
+
+
+def bpe_top_tokens_workspace_bytes(rows: int, n_vocab: int, k: int) -> int:
+    return _check(load_library().bpe_top_tokens_workspace_bytes(int(rows), int(n_vocab), int(k)))
+
+
+def bpe_top_tokens(logits, ids, logprobs, workspace, lse=None, stream=None):
+    """Enqueue ids (int32) and logprobs (float32) [rows, k] = the k best tokens of logits [rows, n_vocab], best first,
+    equal ones by index, -1 behind the last one above -infinity; lse float32 [rows] = log of the sum of exp."""
+    pl, sl, code = _rows(logits, "logits")
+    rows, n_vocab = logits.shape
+    if ids.dim() != 2 or ids.shape[0] != rows or logprobs.shape != ids.shape:
+        raise ValueError(f"ids and logprobs must be [{rows}, k]")
+    _check(load_library().bpe_top_tokens(pl, sl, code, rows, n_vocab, ids.shape[1], _dev_ptr(ids, "int32"), _dev_ptr(logprobs, "float32"),
+                                         None if lse is None else _row_list(lse, "float32", rows, "lse"), _opt_ptr(workspace, "uint8"),
+                                         0 if workspace is None else workspace.numel(), _stream_ptr(stream)))
 
 
 class Pool:

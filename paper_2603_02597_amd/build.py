@@ -10,7 +10,7 @@ ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB_DIR = os.path.join(_HERE, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libbpe_mi355x.so")
-SOURCES = ["bpe_table.hip", "bpe_pretokenize.hip", "bpe_encode.hip", "bpe_vocab.hip"]
+SOURCES = ["bpe_table.hip", "bpe_pretokenize.hip", "bpe_encode.hip", "bpe_vocab.hip", "bpe_grammar.hip", "bpe_logits.hip", "bpe_linear.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # -align-all-nofallthru-blocks=5: a block that is only jumped to starts at a multiple of 32 bytes.  Left to chance,
 # where the merge loops' blocks lie moved calls by 1 % either way with every change elsewhere in a kernel (2 KB
