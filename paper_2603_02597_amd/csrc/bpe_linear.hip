@@ -1,6 +1,7 @@
 // out = activation(x weight^T + bias) + residual on the matrix cores: the projection of hidden states onto a vocabulary,
 // and the small blocks in front of it.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "bpe_numeric.h"
@@ -17,7 +18,9 @@ struct LinearParams {
     int64_t residual_stride;
     void *out;
     int64_t out_stride;
-    int32_t out_dtype;
+    int32_t out_dtype, splits;         // k is cut into so many parts, whose sums meet in `part` if there are several
+    float *part;                       // [splits][m][part_stride]
+    int32_t part_stride;
 };
 
 typedef __bf16 Bf16x8 __attribute__((ext_vector_type(8)));
@@ -43,47 +46,54 @@ __device__ __forceinline__ float activate(float v, int activation) {
     }
 }
 
-// What a call's epilogue is made of; the kernels are compiled for the output's type, the rest are branches that all lanes take together.
-template <class OUT>
-struct Epilogue {
-    const LinearParams &p;
-    __device__ __forceinline__ float finish(int i, int j, float v) const {
-        if (p.bias) v += load_as_float(p.bias, j, p.bias_dtype);
-        v = activate(v, p.activation);
-        if (p.residual) v += to_float<OUT>(((const typename OUT::raw *)p.residual)[i * p.residual_stride + j]);
-        return v;
+typedef float F4Any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint16_t H4Any __attribute__((ext_vector_type(4), aligned(2)));
+
+__device__ __forceinline__ float finish(const LinearParams &p, float v, float bias, float residual) {
+    return activate(v + bias, p.activation) + residual;
+}
+// The epilogue of columns j .. j + 3 of row i, as far as they exist.  (Every lane of a call takes the same branches but the last.)
+__device__ __forceinline__ void put4(const LinearParams &p, int i, int j, F4 v) {
+    const int64_t at = i * p.out_stride + j, from = i * p.residual_stride + j;
+    if (j + 3 >= p.n) {
+#pragma unroll 1
+        for (int e = 0; e < 4 && j + e < p.n; ++e) {
+            const float x = e == 0 ? v[0] : e == 1 ? v[1] : e == 2 ? v[2] : v[3];
+            const float o = finish(p, x, p.bias ? load_as_float(p.bias, j + e, p.bias_dtype) : 0.0f,
+                                   p.residual ? load_as_float(p.residual, from + e, p.out_dtype) : 0.0f);
+            if (p.out_dtype == BPE_F32) ((float *)p.out)[at + e] = o;
+            else ((uint16_t *)p.out)[at + e] = p.out_dtype == BPE_BF16 ? from_float<Bf16>(o) : from_float<F16>(o);
+        }
+        return;
     }
-    __device__ __forceinline__ void put(int i, int j, float v) const {
-        ((typename OUT::raw *)p.out)[i * p.out_stride + j] = from_float<OUT>(finish(i, j, v));
+    if (p.bias) {
+        if (p.bias_dtype == BPE_F32) {
+            v += *(const F4Any *)((const float *)p.bias + j);
+        } else {
+            const H4Any b = *(const H4Any *)((const uint16_t *)p.bias + j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += p.bias_dtype == BPE_BF16 ? to_float<Bf16>(b[e]) : to_float<F16>(b[e]);
+        }
     }
-    // Four neighbours of a row; whole = all four exist.
-    __device__ __forceinline__ void put4(int i, int j, F4 v) const {
-        typedef typename OUT::raw Raw4 __attribute__((ext_vector_type(4), aligned(sizeof(typename OUT::raw))));
-        if (j + 3 >= p.n) {
+    if (p.activation != BPE_ACT_NONE) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (j + e < p.n) put(i, j + e, v[e]);
-            return;
-        }
-        if (p.bias) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += load_as_float(p.bias, j + e, p.bias_dtype);
-        }
-        if (p.activation != BPE_ACT_NONE) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = activate(v[e], p.activation);
-        }
-        if (p.residual) {
-            const Raw4 r = *(const Raw4 *)((const typename OUT::raw *)p.residual + i * p.residual_stride + j);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += to_float<OUT>(r[e]);
-        }
-        Raw4 o;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = from_float<OUT>(v[e]);
-        *(Raw4 *)((typename OUT::raw *)p.out + i * p.out_stride + j) = o;
+        for (int e = 0; e < 4; ++e) v[e] = activate(v[e], p.activation);
     }
-};
+    if (p.out_dtype == BPE_F32) {
+        if (p.residual) v += *(const F4Any *)((const float *)p.residual + from);
+        *(F4Any *)((float *)p.out + at) = v;
+        return;
+    }
+    H4Any o;
+    if (p.residual) {
+        o = *(const H4Any *)((const uint16_t *)p.residual + from);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += p.out_dtype == BPE_BF16 ? to_float<Bf16>(o[e]) : to_float<F16>(o[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = p.out_dtype == BPE_BF16 ? from_float<Bf16>(v[e]) : from_float<F16>(v[e]);
+    *(H4Any *)((uint16_t *)p.out + at) = o;
+}
 
 // Sixteen bytes at any even address: the hardware asks for no more.
 typedef uint32_t U4Any __attribute__((ext_vector_type(4), aligned(2)));
@@ -103,55 +113,64 @@ __device__ __forceinline__ U4 load_tail(const uint16_t *row, int t, int k) {
 // cores' registers and every byte of it is asked for once.  A workgroup takes 16 NT rows of weight, its four wavefronts a
 // quarter of k each (a long row is 4 streams, and a vocabulary of few rows still fills the chip); their sums meet in LDS.
 // weight is the left operand: a lane ends with four neighbouring columns of one row of out.
-constexpr int kRowsAhead = 2;        // steps of 32 columns of k whose loads are under way while one is multiplied
-template <class T, class OUT, int MT, int NT>
+// A step is 64 columns, whole lines of memory: two products, whose loads lie next to each other.
+template <class T, int MT, int NT, int AHEAD>
 __global__ void __launch_bounds__(kGroupThreads) linear_rows_kernel(LinearParams p) {
     __shared__ F4 part[kWavesPerGroup][MT * NT][kWave];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int j0 = blockIdx.x * (16 * NT);
-    const int steps = p.k >> 5, from = (int)((int64_t)steps * wv / kWavesPerGroup), to = (int)((int64_t)steps * (wv + 1) / kWavesPerGroup);
+    const int steps = p.k >> 6, from = (int)((int64_t)steps * wv / kWavesPerGroup), to = (int)((int64_t)steps * (wv + 1) / kWavesPerGroup);
     const uint16_t *w[NT], *x[MT];
 #pragma unroll
     for (int b = 0; b < NT; ++b) w[b] = p.w + min(j0 + 16 * b + (lane & 15), p.n - 1) * p.w_stride + 8 * (lane >> 4);
 #pragma unroll
     for (int a = 0; a < MT; ++a) x[a] = p.x + min(16 * a + (lane & 15), p.m - 1) * p.x_stride + 8 * (lane >> 4);
     F4 acc[MT][NT] = {};
-    U4 wf[kRowsAhead][NT], xf[kRowsAhead][MT];
+    U4 wf[AHEAD][NT][2], xf[AHEAD][MT][2];
     auto load = [&](int u, int step) {
 #pragma unroll
-        for (int b = 0; b < NT; ++b) wf[u][b] = load16(w[b] + 32 * step);
+        for (int b = 0; b < NT; ++b)
 #pragma unroll
-        for (int a = 0; a < MT; ++a) xf[u][a] = load16(x[a] + 32 * step);
-    };
-    auto multiply = [&](int u) {
+            for (int h = 0; h < 2; ++h) wf[u][b][h] = load16(w[b] + 64 * (int64_t)step + 32 * h);
 #pragma unroll
         for (int a = 0; a < MT; ++a)
 #pragma unroll
-            for (int b = 0; b < NT; ++b) acc[a][b] = mma16<T>(wf[u][b], xf[u][a], acc[a][b]);
+            for (int h = 0; h < 2; ++h) xf[u][a][h] = load16(x[a] + 64 * (int64_t)step + 32 * h);
+    };
+    auto multiply = [&](int u) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int a = 0; a < MT; ++a)
+#pragma unroll
+                for (int b = 0; b < NT; ++b) acc[a][b] = mma16<T>(wf[u][b][h], xf[u][a][h], acc[a][b]);
     };
 #pragma unroll
-    for (int u = 0; u < kRowsAhead; ++u)
+    for (int u = 0; u < AHEAD; ++u)
         if (from + u < to) load(u, from + u);
     int step = from;
-    for (; step + 2 * kRowsAhead <= to; step += kRowsAhead)
+    for (; step + 2 * AHEAD <= to; step += AHEAD)
 #pragma unroll
-        for (int u = 0; u < kRowsAhead; ++u) {
+        for (int u = 0; u < AHEAD; ++u) {
             multiply(u);
-            load(u, step + kRowsAhead + u);
+            load(u, step + AHEAD + u);
         }
-    for (; step < to; step += kRowsAhead)
+    for (; step < to; step += AHEAD)
 #pragma unroll
-        for (int u = 0; u < kRowsAhead; ++u)
+        for (int u = 0; u < AHEAD; ++u)
             if (step + u < to) {
                 multiply(u);
-                if (step + kRowsAhead + u < to) load(u, step + kRowsAhead + u);
+                if (step + AHEAD + u < to) load(u, step + AHEAD + u);
             }
-    if (wv == kWavesPerGroup - 1 && (p.k & 31)) {
-        const int t = p.k & ~31;
+    if (wv == kWavesPerGroup - 1 && (p.k & 63)) {
+        const int t = (p.k & ~63) + 8 * (lane >> 4);
 #pragma unroll
-        for (int b = 0; b < NT; ++b) wf[0][b] = load_tail(w[b] - 8 * (lane >> 4), t + 8 * (lane >> 4), p.k);
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int a = 0; a < MT; ++a) xf[0][a] = load_tail(x[a] - 8 * (lane >> 4), t + 8 * (lane >> 4), p.k);
+            for (int b = 0; b < NT; ++b) wf[0][b][h] = load_tail(w[b] - 8 * (lane >> 4), t + 32 * h, p.k);
+#pragma unroll
+            for (int a = 0; a < MT; ++a) xf[0][a][h] = load_tail(x[a] - 8 * (lane >> 4), t + 32 * h, p.k);
+        }
         multiply(0);
     }
 #pragma unroll
@@ -159,13 +178,12 @@ __global__ void __launch_bounds__(kGroupThreads) linear_rows_kernel(LinearParams
 #pragma unroll
         for (int b = 0; b < NT; ++b) part[wv][a * NT + b][lane] = acc[a][b];
     __syncthreads();
-    const Epilogue<OUT> epilogue = {p};
     for (int q = wv; q < MT * NT; q += kWavesPerGroup) {
         F4 v = part[0][q][lane];
 #pragma unroll
         for (int s = 1; s < kWavesPerGroup; ++s) v += part[s][q][lane];
         const int i = 16 * (q / NT) + (lane & 15), j = j0 + 16 * (q % NT) + 4 * (lane >> 4);
-        if (i < p.m && j < p.n) epilogue.put4(i, j, v);
+        if (i < p.m && j < p.n) put4(p, i, j, v);
     }
 }
 
@@ -199,17 +217,20 @@ __device__ __forceinline__ void wait_and_meet() {
 
 // Which tile of out a workgroup makes.  Workgroups go round the eight chiplets by their index, and each chiplet has an L2 of its
 // own: so every chiplet gets a run of neighbouring tiles, eight rows of tiles by as many columns as it takes.
-__device__ __forceinline__ bool tile_of(int64_t tiles_m, int64_t tiles_n, int64_t &tm, int64_t &tn) {
-    const int64_t total = tiles_m * tiles_n, per = (total + 7) / 8, s = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+__device__ __forceinline__ bool tile_of(int64_t tiles_m, int64_t tiles_n, int splits, int64_t &tm, int64_t &tn, int &split) {
+    const int64_t tiles = tiles_m * tiles_n, total = tiles * splits, per = (total + 7) / 8;
+    int64_t s = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
     if ((int64_t)(blockIdx.x >> 3) >= per || s >= total) return false;
+    split = (int)(s / tiles);
+    s %= tiles;
     const int64_t group = s / (8 * tiles_n), rest = s % (8 * tiles_n), high = min<int64_t>(8, tiles_m - 8 * group);
     tm = 8 * group + rest % high;
     tn = rest / high;
     return true;
 }
-static int64_t tile_grid(int64_t tiles_m, int64_t tiles_n) { return (tiles_m * tiles_n + 7) / 8 * 8; }
+static int64_t tile_grid(int64_t tiles_m, int64_t tiles_n, int splits) { return (tiles_m * tiles_n * splits + 7) / 8 * 8; }
 
-template <class T, class OUT, int BM, int BN, int WM, int WN>
+template <class T, int BM, int BN, int WM, int WN, bool DIRECT>
 __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParams p) {
     constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
     constexpr int kLoadsX = BM / 8 / NW, kLoadsW = BN / 8 / NW, kLoads = kLoadsX + kLoadsW;      // of eight rows of 64 columns
@@ -218,22 +239,30 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
     __shared__ __attribute__((aligned(1024))) char lds[2 * kBlock];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int64_t tile_m, tile_n;
-    if (!tile_of((p.m + BM - 1) / BM, (p.n + BN - 1) / BN, tile_m, tile_n)) return;
+    int split;
+    if (!tile_of((p.m + BM - 1) / BM, (p.n + BN - 1) / BN, p.splits, tile_m, tile_n, split)) return;
     const int i0 = (int)tile_m * BM, j0 = (int)tile_n * BN;
     // Sixteen-byte groups of a row lie in LDS at their index XOR the row's last three bits, so that eight neighbouring rows
     // read at one index meet eight different groups of banks.
     const int row8 = lane >> 3, group = (lane & 7) ^ row8;
-    const char *xb = (const char *)(p.x + i0 * p.x_stride), *wb = (const char *)(p.w + j0 * p.w_stride);
+    // this part's blocks of 64 columns; the last part also has what is left behind the last whole block
+    const int all_blocks = p.k >> 6, block0 = (int)((int64_t)all_blocks * split / p.splits), blocks = (int)((int64_t)all_blocks * (split + 1) / p.splits) - block0;
+    const char *xb = (const char *)(p.x + i0 * p.x_stride + 64 * (int64_t)block0), *wb = (const char *)(p.w + j0 * p.w_stride + 64 * (int64_t)block0);
     uint32_t at[kLoads];
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
         const int row = ((q < kLoadsX ? q : q - kLoadsX) * NW + wv) * 8 + row8;
         at[q] = 2u * (uint32_t)((q < kLoadsX ? min(row, p.m - 1 - i0) * (int)p.x_stride : min(row, p.n - 1 - j0) * (int)p.w_stride) + 8 * group);
     }
-    const int blocks = p.k >> 6;
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wv * 1024;
+    U4 held[DIRECT ? 1 : kLoads];      // rows at any alignment pass through registers
     auto load_part = [&](int buf, int t, int q) {
-        load_lds(lds_base + buf + q * (NW * 1024), (q < kLoadsX ? xb : wb) + 128 * (int64_t)t, at[q]);
+        const char *base = (q < kLoadsX ? xb : wb) + 128 * (int64_t)t;
+        if constexpr (DIRECT) load_lds(lds_base + buf + q * (NW * 1024), base, at[q]);
+        else held[q] = load16((const uint16_t *)(base + at[q]));
+    };
+    auto store_part = [&](int buf, int q) {
+        if constexpr (!DIRECT) *(U4 *)(lds + buf + (q * NW + wv) * 1024 + 16 * lane) = held[q];
     };
     const int wm = wv / WN, wn = wv % WN;
     const int xrow = (wm * (BM / WM) + (lane & 31)) * 128, wrow = BM * 128 + (wn * (BN / WN) + (lane & 31)) * 128;
@@ -245,17 +274,18 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
         frag[half][s][f] = *(const U4 *)(lds + (buf + (f < TM ? xrow : wrow) + g) + (f < TM ? f : f - TM) * 4096);
     };
     constexpr int kReads = 2 * (TM + TN), kProducts = 2 * TM * TN;
-    // The products of one half of a block, with the reads of the other half (of the block in `reads`) and, in the second half, the loads
-    // of a later block spread among them.
+    // The products of one half of a block, with the reads of the other half (of the block in `reads`) spread among them, and in the
+    // second half the loads of a later block (what went into registers goes on to `loads` in the first half after).
     auto phase = [&](auto which, int reads, int loads, int t_load) {
         constexpr int half = decltype(which)::value;
 #pragma unroll
         for (int q = 0; q < kProducts; ++q) {
 #pragma unroll
             for (int r = q * kReads / kProducts; r < (q + 1) * kReads / kProducts; ++r) read_part(reads, half ^ 1, r);
-            if constexpr (half == 1) {
 #pragma unroll
-                for (int l = q * kLoads / kProducts; l < (q + 1) * kLoads / kProducts; ++l) load_part(loads, t_load, l);
+            for (int l = q * kLoads / kProducts; l < (q + 1) * kLoads / kProducts; ++l) {
+                if constexpr (half == 1) load_part(loads, t_load, l);
+                else store_part(loads, l);
             }
             const int s = q / (TM * TN), a = q / TN % TM, b = q % TN;
             acc[a][b] = mma32<T>(frag[half][s][TM + b], frag[half][s][a], acc[a][b]);
@@ -265,6 +295,8 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
     if (blocks > 0) {
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) load_part(0, 0, q);
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q) store_part(0, q);
         wait_and_meet();
 #pragma unroll
         for (int q = 0; q < kReads; ++q) read_part(0, 0, q);
@@ -272,7 +304,7 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
         for (int q = 0; q < kLoads; ++q) load_part(kBlock, min(1, blocks - 1), q);
         int mine = 0;
         for (int t = 0; t < blocks; ++t) {
-            phase(std::integral_constant<int, 0>(), mine, 0, 0);
+            phase(std::integral_constant<int, 0>(), mine, mine ^ kBlock, 0);
             wait_and_meet();             // block t + 1 is there, and nobody reads block t any more
             // (behind the last block but one: that block again, for nobody)
             phase(std::integral_constant<int, 1>(), mine ^ kBlock, mine, min(t + 2, blocks - 1));
@@ -281,12 +313,12 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
         wait_and_meet();
     }
     // The columns behind the last whole block, filled up with zeros.
-    if (64 * blocks < p.k) {
+    if (split == p.splits - 1 && (p.k & 63)) {
 #pragma unroll 1
         for (int q = 0; q < kLoads; ++q) {
             const int row = ((q < kLoadsX ? q : q - kLoadsX) * NW + wv) * 8 + row8;
             const uint16_t *from = q < kLoadsX ? p.x + min(i0 + row, p.m - 1) * p.x_stride : p.w + min(j0 + row, p.n - 1) * p.w_stride;
-            *(U4 *)(lds + (q * NW + wv) * 1024 + 16 * lane) = load_tail(from, 64 * blocks + 8 * group, p.k);
+            *(U4 *)(lds + (q * NW + wv) * 1024 + 16 * lane) = load_tail(from, 64 * all_blocks + 8 * group, p.k);
         }
         __syncthreads();
 #pragma unroll
@@ -306,7 +338,6 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
     constexpr int kCols = 32 * TN, kPitch = kCols + 4, kLanesPerRow = kCols / 4;
     static_assert(NW * 32 * kPitch * 4 <= 2 * kBlock, "the rows of all wavefronts fit the buffers");
     float *stage = (float *)lds + wv * (32 * kPitch);
-    const Epilogue<OUT> epilogue = {p};
 #pragma unroll
     for (int a = 0; a < TM; ++a) {
 #pragma unroll
@@ -321,7 +352,10 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
         for (int r = lane / kLanesPerRow; r < 32; r += 64 / kLanesPerRow) {
             const F4 v = *(const F4 *)(stage + r * kPitch + 4 * (lane % kLanesPerRow));
             const int i = i0 + wm * (BM / WM) + 32 * a + r;
-            if (i < p.m && j < p.n) epilogue.put4(i, j, v);
+            if (i < p.m && j < p.n) {
+                if (p.splits > 1) *(F4 *)(p.part + ((int64_t)split * p.m + i) * p.part_stride + j) = v;
+                else put4(p, i, j, v);
+            }
         }
         wave_sync();
     }
@@ -329,12 +363,13 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
 
 // Any alignment and any k: a workgroup of four wavefronts makes 64 x 64 of out, a wavefront 32 x 32 (two by two products of 16 x 16),
 // 32 of k at a time through registers into LDS.
-template <class T, class OUT>
+template <class T>
 __global__ void __launch_bounds__(kGroupThreads) linear_tile_kernel(LinearParams p) {
     __shared__ U4 xs[64][4], ws[64][4];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     int64_t tile_m, tile_n;
-    if (!tile_of((p.m + 63) / 64, (p.n + 63) / 64, tile_m, tile_n)) return;
+    int split;
+    if (!tile_of((p.m + 63) / 64, (p.n + 63) / 64, 1, tile_m, tile_n, split)) return;
     const int i0 = (int)tile_m * 64, j0 = (int)tile_n * 64;
     const int wi = 32 * (wv >> 1), wj = 32 * (wv & 1);
     const uint16_t *xr = p.x + min(i0 + (tid >> 2), p.m - 1) * p.x_stride, *wr = p.w + min(j0 + (tid >> 2), p.n - 1) * p.w_stride;
@@ -350,37 +385,98 @@ __global__ void __launch_bounds__(kGroupThreads) linear_tile_kernel(LinearParams
             for (int b = 0; b < 2; ++b)
                 acc[a][b] = mma16<T>(ws[wj + 16 * b + (lane & 15)][lane >> 4], xs[wi + 16 * a + (lane & 15)][lane >> 4], acc[a][b]);
     }
-    const Epilogue<OUT> epilogue = {p};
 #pragma unroll
     for (int a = 0; a < 2; ++a)
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             const int i = i0 + wi + 16 * a + (lane & 15), j = j0 + wj + 16 * b + 4 * (lane >> 4);
-            if (i < p.m && j < p.n) epilogue.put4(i, j, acc[a][b]);
+            if (i < p.m && j < p.n) put4(p, i, j, acc[a][b]);
         }
 }
 
-template <class T, class OUT>
-static int launch_linear(LinearParams &p, void *stream) {
-    const char *what = "bpe_linear launch";
-    if (p.m <= 64) {
-        const int mt = (p.m + 15) / 16;
-        const int64_t tiles = ((int64_t)p.n + 15) / 16;
-        const int nt = mt == 1 ? 1 : tiles >= 2048 ? 4 : tiles >= 1024 ? 2 : 1;
-        const dim3 grid((unsigned)((tiles + nt - 1) / nt));
-#define ROWS(MT, NT) if (mt == MT && nt == NT) return launch(linear_rows_kernel<T, OUT, MT, NT>, grid, kGroupThreads, p, stream, what)
-        ROWS(1, 1);
-        ROWS(2, 1); ROWS(2, 2); ROWS(2, 4);
-        ROWS(3, 1); ROWS(3, 2); ROWS(3, 4);
-        ROWS(4, 1); ROWS(4, 2); ROWS(4, 4);
-#undef ROWS
+// Adds up the parts of every four neighbours of a row, part by part, and finishes them.
+__global__ void __launch_bounds__(kGroupThreads) linear_join_kernel(LinearParams p) {
+    const int64_t groups = p.part_stride / 4, total = groups * p.m, step = (int64_t)gridDim.x * kGroupThreads;
+    for (int64_t g = (int64_t)blockIdx.x * kGroupThreads + threadIdx.x; g < total; g += step) {
+        const int i = (int)(g / groups), j = 4 * (int)(g % groups);
+        F4 v = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int s = 0; s < p.splits; ++s) v += *(const F4 *)(p.part + ((int64_t)s * p.m + i) * p.part_stride + j);
+        put4(p, i, j, v);
     }
-    const bool direct = p.x_stride % 8 == 0 && p.w_stride % 8 == 0 && !(((uintptr_t)p.x | (uintptr_t)p.w) & 15) &&
-                        p.x_stride < (1 << 21) && p.w_stride < (1 << 21);
-    const int64_t tile = direct ? 256 : 64, grid = tile_grid((p.m + tile - 1) / tile, (p.n + tile - 1) / tile);
+}
+
+// Which tiles a product of these sizes takes, and into how many parts k is cut: what an estimate of the time says.  A tile's
+// row: its sides, how many of its workgroups a compute unit holds, us for a block of 64 columns when a workgroup waits for
+// its loads alone, and the TFLOP/s of the whole chip when nothing else bounds it.
+struct LinearTile { int bm, bn, resident; double block_us, tflops; };
+constexpr LinearTile kLinearTiles[] = {
+    {32, 128, 4, 0.46, 556}, {32, 256, 2, 0.61, 590}, {64, 128, 3, 0.50, 795}, {64, 256, 2, 0.68, 910}, {128, 128, 2, 0.60, 1000}, {256, 256, 1, 1.17, 1210}};
+constexpr int kLinearTileCount = sizeof(kLinearTiles) / sizeof(kLinearTiles[0]);
+struct LinearPlan { int tile, splits; };        // tile -1: linear_rows_kernel
+
+static LinearPlan plan_linear(int64_t m, int64_t n, int64_t k) {
+    // Every wavefront of linear_rows_kernel reads all of x: a row or four, or small weights (1 x 2048 x 2048 6.7 us and in tiles
+    // 11; 16 x 2048 x 2048 6.4 and 11; 16 x 50256 x 1024 26.9 and 20.9; 4 x 100256 x 4096 138 and 141, 8 rows 175 and 147).
+    if (m <= 4 || (m <= 16 && n * k <= (1 << 24))) return {-1, 1};
+    LinearPlan best = {0, 1};
+    double least = 1e300;
+    const double blocks = (double)std::max<int64_t>(k >> 6, 1);
+    for (int t = 0; t < kLinearTileCount; ++t) {
+        const LinearTile &l = kLinearTiles[t];
+        const double tiles = (double)((m + l.bm - 1) / l.bm) * (double)((n + l.bn - 1) / l.bn);
+        for (int splits = 1; splits <= 16; splits *= 2) {
+            if (splits > 1 && (tiles * splits > 768 || blocks < 2 * splits)) break;
+            const double groups = tiles * splits, per = std::ceil(blocks / splits);
+            const double compute = std::ceil(groups / 256) * per * (2.0 * l.bm * l.bn * 64) / (l.tflops * 1e6 / 256);
+            const double wait = std::ceil(groups / (256.0 * l.resident)) * per * l.block_us;
+            // a stream of weights is fastest from one or two workgroups per compute unit; what all tiles load comes through the L2s
+            const double memory = 2.0 * ((double)n * k + (double)m * k) / 5.0e6 * (groups > 512 ? 1.1 : groups < 256 ? 1.5 - groups / 512 : 1.0) +
+                                  2.0 * tiles * (l.bm + l.bn) * k / 4.0e7;
+            const double join = splits > 1 ? 3.0 + (double)splits * m * n * 8 / 4.0e6 : 0.0;
+            const double us = std::max(std::max(compute, wait), memory) + join;
+            if (us < least) { least = us; best = {t, splits}; }
+        }
+    }
+    return best;
+}
+static int64_t part_stride_of(int64_t n) { return (n + 3) & ~3ll; }
+
+template <class T>
+static int launch_linear(LinearParams &p, void *workspace, void *stream) {
+    const char *what = "bpe_linear launch";
+    LinearPlan plan = plan_linear(p.m, p.n, p.k);
+    p.splits = 1;
+    if (plan.tile < 0) return launch(linear_rows_kernel<T, 1, 1, 4>, dim3((unsigned)(((int64_t)p.n + 15) / 16)), kGroupThreads, p, stream, what);
+    // A tile's rows are addressed by 32-bit offsets; rows that lie further apart take the simple kernel.
+    const bool far = p.x_stride >= (1 << 21) || p.w_stride >= (1 << 21);
+    const int64_t bm = far ? 64 : kLinearTiles[plan.tile].bm, bn = far ? 64 : kLinearTiles[plan.tile].bn;
+    p.splits = far ? 1 : plan.splits;
+    const int64_t grid = tile_grid((p.m + bm - 1) / bm, (p.n + bn - 1) / bn, p.splits);
     if (grid > 0x7FFFFFFF) { set_error("bpe_linear: m %d and n %d are too large together", p.m, p.n); return BPE_ERR_SIZE; }
-    if (direct) return launch(linear_block_kernel<T, OUT, 256, 256, 2, 2>, dim3((unsigned)grid), 256, p, stream, what);
-    return launch(linear_tile_kernel<T, OUT>, dim3((unsigned)grid), kGroupThreads, p, stream, what);
+    if (far) return launch(linear_tile_kernel<T>, dim3((unsigned)grid), kGroupThreads, p, stream, what);
+    p.part = (float *)workspace;
+    p.part_stride = (int32_t)part_stride_of(p.n);
+    const bool direct = p.x_stride % 8 == 0 && p.w_stride % 8 == 0 && !(((uintptr_t)p.x | (uintptr_t)p.w) & 15);
+    void (*kernel)(LinearParams) = nullptr;
+#define TILE(INDEX, BM, BN, WM, WN) \
+    case INDEX: \
+        static_assert(kLinearTiles[INDEX].bm == BM && kLinearTiles[INDEX].bn == BN, ""); \
+        kernel = direct ? linear_block_kernel<T, BM, BN, WM, WN, true> : linear_block_kernel<T, BM, BN, WM, WN, false>; \
+        break
+    switch (plan.tile) {
+        TILE(0, 32, 128, 1, 4);
+        TILE(1, 32, 256, 1, 4);
+        TILE(2, 64, 128, 1, 4);
+        TILE(3, 64, 256, 1, 4);
+        TILE(4, 128, 128, 2, 2);
+        TILE(5, 256, 256, 2, 2);
+    }
+#undef TILE
+    const int rc = launch(kernel, dim3((unsigned)grid), kGroupThreads, p, stream, what);
+    if (rc != BPE_OK || p.splits == 1) return rc;
+    const int64_t groups = p.part_stride / 4 * (int64_t)p.m;
+    return launch(linear_join_kernel, dim3((unsigned)std::min<int64_t>((groups + kGroupThreads - 1) / kGroupThreads, 2048)), kGroupThreads, p, stream, what);
 }
 
 }  // namespace bpe
@@ -397,7 +493,8 @@ static int linear_sizes_ok(int64_t m, int64_t n, int64_t k) {
 
 extern "C" int64_t bpe_linear_workspace_bytes(int64_t m, int64_t n, int64_t k) {
     if (!linear_sizes_ok(m, n, k)) return BPE_ERR_SIZE;
-    return 0;
+    const LinearPlan plan = plan_linear(m, n, k);
+    return plan.splits > 1 ? 4 * (int64_t)plan.splits * m * part_stride_of(n) : 0;
 }
 
 extern "C" int bpe_linear(const void *x, int64_t x_stride, const void *weight, int64_t weight_stride, int dtype, int64_t m, int64_t n,
@@ -432,6 +529,5 @@ extern "C" int bpe_linear(const void *x, int64_t x_stride, const void *weight, i
     p.bias = bias; p.bias_dtype = bias_dtype; p.activation = activation;
     p.residual = residual; p.residual_stride = residual_stride;
     p.out = out; p.out_stride = out_stride; p.out_dtype = out_dtype;
-    if (dtype == BPE_BF16) return out_dtype == BPE_F32 ? launch_linear<Bf16, F32>(p, stream) : launch_linear<Bf16, Bf16>(p, stream);
-    return out_dtype == BPE_F32 ? launch_linear<F16, F32>(p, stream) : launch_linear<F16, F16>(p, stream);
+    return dtype == BPE_BF16 ? launch_linear<Bf16>(p, workspace, stream) : launch_linear<F16>(p, workspace, stream);
 }
