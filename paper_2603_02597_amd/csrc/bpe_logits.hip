@@ -1,6 +1,7 @@
 // Logits under the rules of a request (bpe_adjust_logits) and the best tokens of every row (bpe_top_tokens).
 #include <algorithm>
 
+#include "bpe_lookback.h"
 #include "bpe_numeric.h"
 
 namespace bpe {
@@ -76,12 +77,33 @@ __global__ void __launch_bounds__(kGroupThreads) adjust_kernel(AdjustParams p) {
     }
 }
 
+// ---------------------------------------------------------------------------
+// The best tokens of a row, in one pass over it.  A workgroup goes through its part of a row and keeps, in LDS, every logit that
+// may still be among the k best: those not below a bound that at least k logits reach.  The bound is cheap: the threads are put
+// into 2^j >= k sets, and the least of the sets' largest logits so far is reached by one logit of every set.  (Of 8,192 random
+// logits it lets k ln k through, of later ones fewer and fewer.)  What was kept is cut down to the k best by histograms over the
+// range of what is left, and put in order by counting.  Logits are compared as (value, index from behind) in one 64-bit word, so no
+// two are equal and the order in which lanes append does not matter.
+constexpr int kTopThreads = 256, kTopWaves = kTopThreads / kWave;
+constexpr int kTopKeep = 4096;               // words in LDS: four workgroups per compute unit
+constexpr int kTopVectors = 4;               // sixteen-byte loads of a thread that are under way together
+constexpr int kTopBins = 1024;
+constexpr int kTopRank = 256;                // up to so many words are put in order by counting
+constexpr int kMaxTop = 256;
+constexpr float kLog2E = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// What a part leaves: its largest logit, the sum of exp(logit - largest), a bound that k of its words reach, the number of its words.
+struct TopPart { float largest, sum, bound; int32_t words; };
+
 struct TopParams {
     const void *logits;
     int64_t logits_stride;
-    int32_t rows, n_vocab, k;
+    int32_t rows, n_vocab, k, sets;          // sets: power of two, k <= sets <= kTopThreads
+    int32_t parts, part_len, part_keep;      // a row is cut into so many parts of part_len logits, each leaves up to part_keep words
     int32_t *ids;
     float *logprobs, *lse;
+    uint64_t *kept;                          // [rows][parts][part_keep] words of a part, among them its k best
+    struct TopPart *left;                    // [rows][parts]
 };
 
 // Floats as unsigned numbers in the same order; both zeros are one value, every NaN the largest.
@@ -93,52 +115,356 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 __device__ __forceinline__ float key_value(uint32_t key) {
     return key == 0xFFFFFFFFu ? __builtin_nanf("") : __builtin_bit_cast(float, key & 0x80000000u ? key ^ 0x80000000u : ~key);
 }
+__device__ __forceinline__ uint64_t top_word(float x, int v) { return (uint64_t)order_key(x) << 32 | ~(uint32_t)v; }
 
-// A workgroup takes a row and finds its best token, the best of the rest and so on: k passes.
-template <class IN>
-__global__ void __launch_bounds__(1024) top_kernel(TopParams p) {
-    __shared__ uint64_t best_of[16];
-    __shared__ float sum_of[16];
+struct TopShared {
+    uint64_t word[kTopKeep];
+    uint32_t bin[kTopBins];
+    uint64_t few[kTopRank];
+    float wave_value[kTopWaves];
+    float2 wave_sum[kTopWaves];
+    uint64_t low, high;
+    int n, n_few, above;
+};
+
+// A bound that at least k of the `count` words reach and at most kTopRank: a histogram over [low, high], then over the range of the
+// bin that the k-th word is in, and so on (each a 1,024th of the one before, so there are at most seven).  No word is above `high`; of
+// those from `low` on there are at least k, or else the bound is `low`.
+__device__ __forceinline__ uint64_t bound_of_best(TopShared &sh, int count, int k, uint64_t low, uint64_t high) {
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    for (int row = blockIdx.x; row < p.rows; row += gridDim.x) {
-        const typename IN::raw *in = (const typename IN::raw *)p.logits + row * p.logits_stride;
-        uint64_t bound = ~0ull;                    // (key, ~index) of the one found last
-        float lse = 0.0f;
-        for (int j = 0; j < p.k; ++j) {
-            uint64_t best = 0;
-            for (int v = tid; v < p.n_vocab; v += 1024) {
-                const uint64_t e = (uint64_t)order_key(to_float<IN>(in[v])) << 32 | ~(uint32_t)v;
-                if (e < bound && e > best) best = e;
-            }
-            for (int d = 32; d; d >>= 1) {
-                const uint64_t o = __shfl_xor((unsigned long long)best, d);
-                best = o > best ? o : best;
-            }
-            __syncthreads();
-            if (lane == 0) best_of[wv] = best;
-            __syncthreads();
-            for (int w = 0; w < 16; ++w) best = best_of[w] > best ? best_of[w] : best;
-            bound = best;
-            const float x = key_value((uint32_t)(best >> 32));
-            if (j == 0) {
-                float sum = 0.0f;
-                const float most = x == -__builtin_inff() ? 0.0f : x;
-                for (int v = tid; v < p.n_vocab; v += 1024) sum += expf(to_float<IN>(in[v]) - most);
-                for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-                if (lane == 0) sum_of[wv] = sum;
-                __syncthreads();
-                sum = 0.0f;
-                for (int w = 0; w < 16; ++w) sum += sum_of[w];
-                lse = x == __builtin_inff() ? x : x + logf(sum);
-                if (p.lse && tid == 0) p.lse[row] = lse;
-            }
-            if (tid == 0) {
-                const bool none = x == -__builtin_inff();
-                p.ids[(int64_t)row * p.k + j] = none ? -1 : (int)~(uint32_t)best;
-                p.logprobs[(int64_t)row * p.k + j] = none ? x : x - lse;
+    if (count <= kTopRank) return 0;
+    int above = 0;                            // words above `high`: fewer than k
+    for (;;) {
+        const int shift = max(0, 54 - __builtin_clzll((high - low) | 1));        // (high - low) >> shift < kTopBins
+        for (int i = tid; i < kTopBins; i += kTopThreads) sh.bin[i] = 0;
+        __syncthreads();
+        for (int i = tid; i < count; i += kTopThreads) {
+            const uint64_t w = sh.word[i];
+            if (w >= low && w <= high) atomicAdd(&sh.bin[(w - low) >> shift], 1u);
+        }
+        __syncthreads();
+        if (wv == 0) {
+            if (lane == 0) sh.n_few = 0;      // (unless a lane finds the k-th word below)
+            // a lane takes 16 bins, the highest ones first: words in the bins of the lanes before it, then in its own
+            constexpr int kPer = kTopBins / kWave;
+            uint32_t in[kPer], mine = 0;
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) mine += in[q] = sh.bin[kTopBins - 1 - (lane * kPer + q)];
+            uint32_t before = wave_scan_inclusive((int)mine) + above - mine;
+            if (before < (uint32_t)k && before + mine >= (uint32_t)k) {          // one lane: the k-th word is in one of its bins
+                int bin = 0;
+                uint32_t there = 0;
+                bool found = false;
+#pragma unroll
+                for (int q = 0; q < kPer; ++q) {
+                    if (!found && before + in[q] >= (uint32_t)k) {
+                        found = true;
+                        bin = kTopBins - 1 - (lane * kPer + q);
+                        there = in[q];
+                    }
+                    if (!found) before += in[q];
+                }
+                sh.low = low + ((uint64_t)bin << shift);
+                const uint64_t end = sh.low + (((uint64_t)1 << shift) - 1);
+                sh.high = end < high ? end : high;
+                sh.above = (int)before;
+                sh.n_few = (int)(before + there);
             }
         }
+        __syncthreads();
+        if (sh.n_few == 0) return low;
+        low = sh.low;
+        high = sh.high;
+        above = sh.above;
+        if (sh.n_few <= kTopRank) return low;
+        __syncthreads();
     }
+}
+
+// The k best of the `count` words, best first, to place(rank, word); returns how many there are.  low, high: see bound_of_best.
+template <class Place>
+__device__ __forceinline__ int place_best(TopShared &sh, int count, int k, uint64_t low, uint64_t high, Place place) {
+    const int tid = threadIdx.x;
+    const uint64_t bound = bound_of_best(sh, count, k, low, high);
+    __syncthreads();
+    if (tid == 0) sh.n_few = 0;
+    sh.few[tid] = 0;
+    __syncthreads();
+    for (int i = tid; i < count; i += kTopThreads) {
+        const uint64_t w = sh.word[i];
+        if (w >= bound) sh.few[atomicAdd(&sh.n_few, 1)] = w;
+    }
+    __syncthreads();
+    // Several threads to a word count how many of a part of the words are larger.
+    const int n = sh.n_few, slots = n <= 32 ? 32 : n <= 64 ? 64 : n <= 128 ? 128 : 256, per = kTopThreads / slots;
+    const uint64_t w = sh.few[tid / per];
+    typedef uint64_t Words __attribute__((ext_vector_type(2)));
+    const Words *others = (const Words *)sh.few + tid % per * (slots / per / 2);
+    int rank = 0;
+#pragma unroll 8
+    for (int o = 0; o < slots / per / 2; ++o) {
+        const Words v = others[o];
+        rank += (v[0] > w) + (v[1] > w);
+    }
+    for (int d = 1; d < per; d <<= 1) rank += __shfl_xor(rank, d);
+    if (tid % per == 0 && w && rank < k) place(rank, w);
+    return min(n, k);
+}
+static_assert(kTopRank == kTopThreads, "a thread per word");
+
+template <int CTRL> __device__ __forceinline__ float dpp(float v) {
+    const int u = __builtin_bit_cast(int, v);
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(u, u, CTRL, 0xF, 0xF, false));
+}
+// The value of the lane whose index differs in bit DISTANCE, or of another one of its group of DISTANCE lanes, which are all alike here.
+template <int DISTANCE> __device__ __forceinline__ float other_group(float v) {
+    if constexpr (DISTANCE == 1) return dpp<0xB1>(v);         // quad_perm 1 0 3 2
+    else if constexpr (DISTANCE == 2) return dpp<0x4E>(v);    // quad_perm 2 3 0 1
+    else if constexpr (DISTANCE == 4) return dpp<0x141>(v);   // row_half_mirror
+    else if constexpr (DISTANCE == 8) return dpp<0x140>(v);   // row_mirror
+    else return __shfl_xor(v, DISTANCE);
+}
+template <int DISTANCE, class Op> __device__ __forceinline__ float join_groups(float v, Op op) { return op(v, other_group<DISTANCE>(v)); }
+template <class Op> __device__ __forceinline__ float wave_join(float v, Op op) {
+    v = join_groups<1>(v, op);
+    v = join_groups<2>(v, op);
+    v = join_groups<4>(v, op);
+    v = join_groups<8>(v, op);
+    v = join_groups<16>(v, op);
+    return join_groups<32>(v, op);
+}
+
+__device__ __forceinline__ float in_or_between(float a, float b, bool in_a_set) { return in_a_set ? fmaxf(a, b) : fminf(a, b); }
+// The least of the sets' largest values: reached by a logit of every set.  A set is `together` neighbouring threads, a power of two.
+__device__ __forceinline__ float least_of_sets(TopShared &sh, float largest, int sets) {
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    const int together = kTopThreads / sets;
+    float v = largest;
+    v = in_or_between(v, other_group<1>(v), 1 < together);
+    v = in_or_between(v, other_group<2>(v), 2 < together);
+    v = in_or_between(v, other_group<4>(v), 4 < together);
+    v = in_or_between(v, other_group<8>(v), 8 < together);
+    v = in_or_between(v, other_group<16>(v), 16 < together);
+    v = in_or_between(v, other_group<32>(v), 32 < together);
+    if (lane == 0) sh.wave_value[wv] = v;
+    __syncthreads();
+    static_assert(kTopWaves == 4, "");
+    const float a = in_or_between(sh.wave_value[0], sh.wave_value[1], 64 < together), b = in_or_between(sh.wave_value[2], sh.wave_value[3], 64 < together);
+    return in_or_between(a, b, 128 < together);
+}
+
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
+// What exp(x - largest) is taken against: a row of -infinity has no other.
+__device__ __forceinline__ float reference_of(float largest) { return largest == -__builtin_inff() ? 0.0f : largest; }
+
+// {largest, sum} of the whole workgroup, in a fixed order.
+__device__ __forceinline__ float2 join_sums(TopShared &sh, float largest, float sum) {
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    const float m = wave_join(largest, [](float a, float b) { return fmaxf(a, b); });
+    sum = wave_join(sum * exp_of(largest - reference_of(m)), [](float a, float b) { return a + b; });
+    if (lane == 0) sh.wave_sum[wv] = make_float2(m, sum);
+    __syncthreads();
+    float all = -__builtin_inff(), s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kTopWaves; ++w) all = fmaxf(all, sh.wave_sum[w].x);
+#pragma unroll
+    for (int w = 0; w < kTopWaves; ++w) s += sh.wave_sum[w].y * exp_of(sh.wave_sum[w].x - reference_of(all));
+    return make_float2(all, s);
+}
+
+// log of the sum: NaN if the best logit is one, +infinity if that is; `best`: the word of the best one, 0 if there is none.
+__device__ __forceinline__ float log_sum(float2 total, uint64_t best) {
+    const float x = best ? key_value((uint32_t)(best >> 32)) : -__builtin_inff();
+    if (x != x || x == __builtin_inff() || x == -__builtin_inff()) return x;
+    return total.x + __builtin_amdgcn_logf(total.y) * kLn2;
+}
+
+// Words from that of a logit on, and up to it; a sum that is NaN leaves open what the largest is.
+__device__ __forceinline__ uint64_t words_from(float x) { return (uint64_t)order_key(x) << 32; }
+__device__ __forceinline__ uint64_t words_to(float2 total) { return total.y != total.y ? ~0ull : words_from(total.x) | 0xFFFFFFFFu; }
+
+__device__ __forceinline__ void write_row(const TopParams &p, TopShared &sh, int row, int count, uint64_t low, float2 total) {
+    const int tid = threadIdx.x;
+    const int n = place_best(sh, count, p.k, low, words_to(total), [&](int rank, uint64_t w) {
+        sh.word[rank] = w;                                // (every word that is still needed is in sh.few)
+    });
+    __syncthreads();
+    const float lse = log_sum(total, n ? sh.word[0] : 0);
+    if (p.lse && tid == 0) p.lse[row] = lse;
+    for (int j = tid; j < p.k; j += kTopThreads) {
+        const uint64_t w = j < n ? sh.word[j] : 0;
+        const float x = key_value((uint32_t)(w >> 32));
+        p.ids[(int64_t)row * p.k + j] = j < n ? (int)~(uint32_t)w : -1;
+        p.logprobs[(int64_t)row * p.k + j] = j < n ? x - lse : -__builtin_inff();
+    }
+}
+
+template <class IN>
+__global__ void __launch_bounds__(kTopThreads, 4) top_part_kernel(TopParams p) {
+    constexpr int kPer = 16 / (int)sizeof(typename IN::raw), kRound = kTopThreads * kPer * kTopVectors;
+    typedef typename IN::raw Vec __attribute__((ext_vector_type(kPer), aligned(sizeof(typename IN::raw))));
+    __shared__ TopShared sh;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int row = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
+    const int first = part * p.part_len, last = min(first + p.part_len, p.n_vocab);
+    const typename IN::raw *in = (const typename IN::raw *)p.logits + row * p.logits_stride;
+    if (tid == 0) sh.n = 0;
+    float largest = -__builtin_inff(), sum = 0.0f;
+    float bound = -3.402823466e38f;                       // logits below it are out; so is -infinity
+    uint64_t bound_word = 0;                              // and words that are not above this one
+    int before = 0, n_rounds = 0;
+    for (int at = first; at < last; at += kRound, ++n_rounds) {
+        float x[kTopVectors][kPer];
+#pragma unroll
+        for (int q = 0; q < kTopVectors; ++q) {
+            const int v = at + (q * kTopThreads + tid) * kPer;
+            if (v + kPer <= last) {
+                const Vec t = *(const Vec *)(in + v);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) x[q][e] = to_float<IN>(t[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) x[q][e] = -__builtin_inff();
+                if (v < last) {                           // one thread of a row at most
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e)
+                        if (v + e < last) x[q][e] = to_float<IN>(in[v + e]);
+                }
+            }
+        }
+        float m = largest;
+#pragma unroll
+        for (int q = 0; q < kTopVectors; ++q)
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) m = fmaxf(m, x[q][e]);
+        const float ref = reference_of(m);
+        sum *= exp_of(largest - ref);
+#pragma unroll
+        for (int q = 0; q < kTopVectors; ++q)
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) sum += exp_of(x[q][e] - ref);
+        largest = m;
+        const float bound_before = bound;                 // reached by k of the words that are there
+        if ((n_rounds & (n_rounds + 1)) == 0) bound = fmaxf(bound, least_of_sets(sh, largest, p.sets));   // rounds 0, 1, 3, 7, ...
+        else __syncthreads();
+        // A lane's logits that stay, one bit each: few, so they are read again.
+        uint32_t stay = 0;
+#pragma unroll
+        for (int q = 0; q < kTopVectors; ++q)
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) stay |= x[q][e] < bound ? 0u : 1u << (q * kPer + e);
+        auto word_of = [&](int bit) {
+            const int v = at + (bit / kPer * kTopThreads + tid) * kPer + bit % kPer;
+            return top_word(to_float<IN>(in[v]), v);
+        };
+        // A wavefront takes room for all of its lanes' at once.  Beyond kTopKeep they are only counted.
+        if (__ballot(stay != 0)) {
+            const int mine = __builtin_popcount(stay), up_to = wave_scan_inclusive(mine);
+            int base = 0;
+            if (lane == kWave - 1) base = atomicAdd(&sh.n, up_to);
+            int to = up_to - mine + __builtin_amdgcn_readlane(base, kWave - 1);
+            for (uint32_t left = stay; left; left &= left - 1, ++to)
+                if (to < kTopKeep) sh.word[to] = word_of(__builtin_ctz(left));
+        }
+        __syncthreads();
+        const int n = sh.n;
+        if (n <= kTopKeep) { before = n; continue; }
+        // More than there is room for: what this round has appended is taken back, the words cut down to the k best, and the
+        // round's logits looked at again, one of every thread at a time, with another cut whenever room runs out.
+        int count = before;
+        auto cut = [&]() {
+            const int left = place_best(sh, count, p.k, words_from(bound_before), ~0ull, [&](int rank, uint64_t w) { sh.word[rank] = w; });
+            __syncthreads();
+            if (left == p.k) bound_word = sh.word[p.k - 1];
+            if (tid == 0) sh.n = left;
+            __syncthreads();
+            count = left;
+        };
+        cut();
+        for (int bit = 0; bit < kTopVectors * kPer; ++bit) {
+            if (count > kTopKeep - kTopThreads) cut();
+            if (stay >> bit & 1u) {
+                const uint64_t w = word_of(bit);
+                if (w > bound_word) sh.word[atomicAdd(&sh.n, 1)] = w;
+            }
+            __syncthreads();
+            count = sh.n;
+            __syncthreads();
+        }
+        before = count;
+        if (bound_word) bound = fmaxf(bound, key_value((uint32_t)(bound_word >> 32)));
+    }
+    __syncthreads();
+    const float2 total = join_sums(sh, largest, sum);
+    if (n_rounds > 1) bound = fmaxf(bound, least_of_sets(sh, largest, p.sets));
+    if (p.parts == 1) {
+        write_row(p, sh, row, before, words_from(bound), total);
+        return;
+    }
+    // The words above the bound go to the workgroup that joins the parts; if they are too many, the k best.
+    TopPart &left = p.left[(int64_t)row * p.parts + part];
+    uint64_t *out = p.kept + ((int64_t)row * p.parts + part) * p.part_keep;
+    const uint64_t low = words_from(bound);
+    int n = before;
+    if (n_rounds > 1) {                                   // (after one round all words are above the bound)
+        if (tid == 0) sh.n_few = 0;
+        __syncthreads();
+        for (int i = tid; i < before; i += kTopThreads) {
+            const uint64_t w = sh.word[i];
+            if (w >= low) {
+                const int to = atomicAdd(&sh.n_few, 1);
+                if (to < p.part_keep) out[to] = w;
+            }
+        }
+        __syncthreads();
+        n = sh.n_few;
+    } else if (n <= p.part_keep) {
+        for (int i = tid; i < n; i += kTopThreads) out[i] = sh.word[i];
+    }
+    if (n > p.part_keep) {
+        __syncthreads();
+        n = place_best(sh, before, p.k, low, words_to(total), [&](int rank, uint64_t w) { out[rank] = w; });
+    }
+    if (tid == 0) left = {total.x, total.y, bound, n};
+}
+
+// The best of the parts' best: none is below the highest of the parts' bounds.
+__global__ void __launch_bounds__(kTopThreads) top_join_kernel(TopParams p) {
+    __shared__ TopShared sh;
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, row = blockIdx.x;
+    const TopPart *left = p.left + (int64_t)row * p.parts;
+    float bound = -3.402823466e38f, largest = -__builtin_inff(), sum = 0.0f;
+    for (int i = tid; i < p.parts; i += kTopThreads) {
+        const TopPart t = left[i];
+        const float m = fmaxf(largest, t.largest), ref = reference_of(m);
+        sum = sum * exp_of(largest - ref) + t.sum * exp_of(t.largest - ref);
+        largest = m;
+        bound = fmaxf(bound, t.bound);
+    }
+    bound = wave_join(bound, [](float a, float b) { return fmaxf(a, b); });
+    if (lane == 0) sh.wave_value[wv] = bound;
+    if (tid == 0) sh.n = 0;
+    const float2 total = join_sums(sh, largest, sum);
+#pragma unroll
+    for (int w = 0; w < kTopWaves; ++w) bound = fmaxf(bound, sh.wave_value[w]);
+    const uint64_t low = words_from(bound);
+    const uint64_t *in = p.kept + (int64_t)row * p.parts * p.part_keep;
+    // a power of two of threads to every part, four of its words at a time
+    int per = kTopThreads;
+    while (per > 1 && per * p.parts > kTopThreads) per /= 2;
+    for (int part = tid / per; part < p.parts; part += kTopThreads / per) {
+        const int n = left[part].words;
+        for (int i = tid % per; i < n; i += 4 * per) {
+            uint64_t w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) w[q] = i + q * per < n ? in[(int64_t)part * p.part_keep + i + q * per] : 0;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (w[q] >= low && w[q]) sh.word[atomicAdd(&sh.n, 1)] = w[q];
+        }
+    }
+    __syncthreads();
+    write_row(p, sh, row, sh.n, low, total);
 }
 
 }  // namespace bpe
@@ -200,8 +526,6 @@ extern "C" int bpe_adjust_logits(const void *logits, int64_t logits_stride, int 
     return launch(kernel, grid, kGroupThreads, p, stream, "bpe_adjust_logits launch");
 }
 
-constexpr int64_t kMaxTop = 256;
-
 static int check_top(int64_t rows, int64_t n_vocab, int64_t k) {
     const int rc = check_rows("bpe_top_tokens", rows, n_vocab, BPE_F32);
     if (rc != BPE_OK) return rc;
@@ -209,9 +533,21 @@ static int check_top(int64_t rows, int64_t n_vocab, int64_t k) {
     return BPE_OK;
 }
 
+static int64_t align256l(int64_t v) { return (v + 255) & ~255ll; }
+
+// Parts of a row: four workgroups per compute unit in all, none of fewer than 4,096 logits, and no more words than one workgroup joins.
+static int64_t top_parts(int64_t rows, int64_t n_vocab, int64_t k) {
+    const int64_t parts = std::min(std::min((1024 + rows - 1) / std::max<int64_t>(rows, 1), (n_vocab + 4095) / 4096), (int64_t)kTopKeep / k);
+    return std::max<int64_t>(parts, 1);
+}
+// Words that a part leaves: k ln k of a part of one round are above its bound as a rule.
+static int64_t part_keep(int64_t parts, int64_t k) { return std::min<int64_t>(std::max<int64_t>(8 * k, 32), kTopKeep / parts); }
+
 extern "C" int64_t bpe_top_tokens_workspace_bytes(int64_t rows, int64_t n_vocab, int64_t k) {
     const int rc = check_top(rows, n_vocab, k);
-    return rc != BPE_OK ? rc : 0;
+    if (rc != BPE_OK) return rc;
+    const int64_t parts = top_parts(rows, n_vocab, k);
+    return parts > 1 ? align256l(8 * rows * parts * part_keep(parts, k)) + (int64_t)sizeof(TopPart) * rows * parts : 0;
 }
 
 extern "C" int bpe_top_tokens(const void *logits, int64_t logits_stride, int dtype, int64_t rows, int64_t n_vocab, int64_t k,
@@ -236,6 +572,16 @@ extern "C" int bpe_top_tokens(const void *logits, int64_t logits_stride, int dty
     p.ids = ids;
     p.logprobs = logprobs;
     p.lse = lse;
-    return launch(dtype == BPE_F32 ? top_kernel<F32> : dtype == BPE_BF16 ? top_kernel<Bf16> : top_kernel<F16>,
-                  dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), 1024, p, stream, "bpe_top_tokens launch");
+    for (p.sets = 1; p.sets < p.k;) p.sets *= 2;
+    const int64_t parts = top_parts(rows, n_vocab, k);
+    if (rows * parts > 0x7FFFFFFF) { set_error("bpe_top_tokens: rows out of range (%lld)", (long long)rows); return BPE_ERR_SIZE; }
+    p.parts = (int32_t)parts;
+    p.part_len = (int32_t)(((n_vocab + parts - 1) / parts + 7) & ~7ll);
+    p.kept = (uint64_t *)workspace;
+    p.part_keep = (int32_t)part_keep(parts, k);
+    p.left = (TopPart *)((char *)workspace + align256l(8 * rows * parts * p.part_keep));
+    const int rc = launch(dtype == BPE_F32 ? top_part_kernel<F32> : dtype == BPE_BF16 ? top_part_kernel<Bf16> : top_part_kernel<F16>,
+                          dim3((unsigned)(rows * parts)), kTopThreads, p, stream, "bpe_top_tokens launch");
+    if (rc != BPE_OK || parts == 1) return rc;
+    return launch(top_join_kernel, dim3((unsigned)rows), kTopThreads, p, stream, "bpe_top_tokens launch");
 }
