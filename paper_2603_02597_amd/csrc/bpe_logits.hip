@@ -11,6 +11,7 @@ struct AdjustParams {
     void *out;
     int64_t logits_stride, out_stride;
     int32_t rows, n_vocab;
+    int32_t slice, slices;             // tokens of a row per workgroup, a multiple of 32
     bpe_logit_rules rules;
 };
 
@@ -22,8 +23,6 @@ __device__ __forceinline__ void row_range(const int32_t *offsets, int64_t n, int
     end = min(max(offsets[row + 1], begin), (int)n);
 }
 
-constexpr int kSlice = 4096;         // tokens of a row per workgroup
-
 // The row's mask, or nullptr; `nothing` if its index is too large.
 __device__ __forceinline__ const uint32_t *row_mask(const bpe_logit_rules &r, int row, bool &nothing) {
     nothing = false;
@@ -34,45 +33,125 @@ __device__ __forceinline__ const uint32_t *row_mask(const bpe_logit_rules &r, in
     return nothing ? nullptr : r.masks + i * r.mask_stride;
 }
 
-// A workgroup takes a slice of a row: it counts the row's history and notes its biases in LDS, then makes one pass over the slice.
-template <class IN, class OUT>
-__global__ void __launch_bounds__(kGroupThreads) adjust_kernel(AdjustParams p) {
+// A workgroup takes a slice of a row.  With LISTS it first counts the row's history in LDS and marks the biased tokens, then makes one
+// pass over the slice, sixteen bytes per lane; the biased tokens, which that pass leaves out, come last.  Every slice of a row
+// reads the row's whole history: slices are as long as LDS allows with two workgroups per compute unit.
+constexpr int kAdjustThreads = 512, kAdjustSlice = 16384;
+constexpr uint32_t kBiased = 0x80000000u;             // in a count
+template <class IN, class OUT, bool LISTS>
+__global__ void __launch_bounds__(kAdjustThreads) adjust_kernel(AdjustParams p) {
 #pragma clang fp contract(off)
-    __shared__ uint32_t count[kSlice], bias_at[kSlice];
+    constexpr int kPer = 16 / (int)sizeof(typename IN::raw);
+    typedef typename IN::raw InVec __attribute__((ext_vector_type(kPer), aligned(sizeof(typename IN::raw))));
+    typedef typename OUT::raw OutVec __attribute__((ext_vector_type(kPer), aligned(sizeof(typename OUT::raw))));
+    typedef int32_t Int4Any __attribute__((ext_vector_type(4), aligned(4)));
+    typedef uint32_t Counts __attribute__((ext_vector_type(kPer)));
+    __shared__ __attribute__((aligned(32))) uint32_t count[LISTS ? kAdjustSlice : 1];
     const bpe_logit_rules &r = p.rules;
-    const int first = blockIdx.x * kSlice, last = min(first + kSlice, p.n_vocab), tid = threadIdx.x;
-    for (int row = blockIdx.y; row < p.rows; row += gridDim.y) {
-        __syncthreads();
-        for (int i = tid; i < kSlice; i += kGroupThreads) count[i] = bias_at[i] = 0;
-        __syncthreads();
+    const int row = blockIdx.x / p.slices, first = blockIdx.x % p.slices * p.slice, last = min(first + p.slice, p.n_vocab), tid = threadIdx.x;
+    const typename IN::raw *in = (const typename IN::raw *)p.logits + row * p.logits_stride;
+    typename OUT::raw *out = (typename OUT::raw *)p.out + row * p.out_stride;
+    int bias_begin = 0, bias_end = 0;
+    float rep = 1.0f, freq = 0.0f, pres = 0.0f;
+    auto punished = [&](float x, uint32_t c) {
+        x = x > 0.0f ? x / rep : x * rep;
+        x = x - freq * (float)c;
+        return x - pres;
+    };
+    if constexpr (LISTS) {
+        for (int i = 4 * tid; i < p.slice; i += 4 * kAdjustThreads) *(U4 *)(count + i) = U4{0, 0, 0, 0};
+        rep = r.repetition ? r.repetition[row] : 1.0f;
+        freq = r.frequency ? r.frequency[row] : 0.0f;
+        pres = r.presence ? r.presence[row] : 0.0f;
         int begin, end;
         row_range(r.history_offsets, r.n_history, row, begin, end);
-        for (int i = begin + tid; i < end; i += kGroupThreads) {
-            const int v = r.history[i];
+        row_range(r.bias_offsets, r.n_bias, row, bias_begin, bias_end);
+        __syncthreads();
+        auto note = [&](int v) {
             if (v >= first && v < last) atomicAdd(&count[v - first], 1u);
+        };
+        int i = begin + 4 * tid;
+        for (; i <= end - 4; i += 4 * kAdjustThreads) {
+            const Int4Any v = *(const Int4Any *)(r.history + i);
+            note(v[0]); note(v[1]); note(v[2]); note(v[3]);
         }
-        row_range(r.bias_offsets, r.n_bias, row, begin, end);
-        for (int i = begin + tid; i < end; i += kGroupThreads) {
+        for (; i < end; ++i) note(r.history[i]);          // (one thread's: the last one to three)
+        for (int i = bias_begin + tid; i < bias_end; i += kAdjustThreads) {
             const int v = r.bias_ids[i];
-            if (v >= first && v < last) atomicMax(&bias_at[v - first], (uint32_t)i + 1u);     // the last entry counts
+            if (v >= first && v < last) atomicOr(&count[v - first], kBiased);
         }
         __syncthreads();
-        const float rep = r.repetition ? r.repetition[row] : 1.0f, freq = r.frequency ? r.frequency[row] : 0.0f,
-                    pres = r.presence ? r.presence[row] : 0.0f;
-        bool nothing;
-        const uint32_t *mask = row_mask(r, row, nothing);
-        const typename IN::raw *in = (const typename IN::raw *)p.logits + row * p.logits_stride;
-        typename OUT::raw *out = (typename OUT::raw *)p.out + row * p.out_stride;
-        for (int v = first + tid; v < last; v += kGroupThreads) {
-            float x = to_float<IN>(in[v]);
-            if (const uint32_t c = count[v - first]) {
-                x = x > 0.0f ? x / rep : x * rep;
-                x = x - freq * (float)c;
-                x = x - pres;
+    }
+    bool nothing;
+    const uint32_t *mask = row_mask(r, row, nothing);
+    for (int v = first + kPer * tid; v < last; v += kPer * kAdjustThreads) {
+        const bool whole = v + kPer <= last;
+        InVec t;
+        if (whole) {
+            t = *(const InVec *)(in + v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) t[e] = v + e < last ? in[v + e] : typename IN::raw(0);
+        }
+        uint32_t allowed = nothing ? 0u : ~0u, biased = 0;
+        if (mask) allowed = mask[v >> 5] >> (v & 31);
+        float x[kPer];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) x[e] = to_float<IN>(t[e]);
+        if constexpr (LISTS) {
+            const Counts c = *(const Counts *)(count + (v - first));
+            uint32_t any = 0;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) any |= c[e];
+            if (any) {
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) {
+                    if (c[e] & ~kBiased) x[e] = punished(x[e], c[e]);
+                    biased |= c[e] >> 31 << e;
+                }
             }
-            if (const uint32_t b = bias_at[v - first]) x = x + r.bias_values[b - 1];
-            if (nothing || (mask && !((mask[v >> 5] >> (v & 31)) & 1u))) x = -__builtin_inff();
-            out[v] = from_float<OUT>(x);
+        }
+        OutVec o;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[e] = from_float<OUT>(allowed >> e & 1u ? x[e] : -__builtin_inff());
+        if (whole && !biased) {
+            *(OutVec *)(out + v) = o;
+        } else {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+                if (v + e < last && !(biased >> e & 1u)) out[v + e] = o[e];
+        }
+    }
+    if constexpr (LISTS) {
+        // The biased tokens, the list from its end: an entry whose token is still marked counts, of several of one token among those
+        // at hand the last one.  (A marked token's logit has not been written yet, also in place.)
+        for (int back = bias_end; back > bias_begin; back -= kAdjustThreads) {
+            __syncthreads();
+            const int i = back - 1 - tid;
+            int v = -1;
+            uint32_t c = 0;
+            if (i >= bias_begin) {
+                v = r.bias_ids[i];
+                v = v >= first && v < last ? v - first : -1;
+                if (v >= 0) c = count[v];
+                if (!(c & kBiased)) v = -1;
+            }
+            __syncthreads();
+            if (v >= 0) count[v] = 0;
+            __syncthreads();
+            if (v >= 0) atomicMax(&count[v], (uint32_t)(kAdjustThreads - tid));
+            __syncthreads();
+            const bool mine = v >= 0 && count[v] == (uint32_t)(kAdjustThreads - tid);
+            __syncthreads();
+            if (mine) {
+                c &= ~kBiased;
+                count[v] = c;
+                float x = to_float<IN>(in[first + v]);
+                if (c) x = punished(x, c);
+                x = x + r.bias_values[i];
+                const bool keep = mask ? (mask[(first + v) >> 5] >> ((first + v) & 31)) & 1u : !nothing;
+                out[first + v] = from_float<OUT>(keep ? x : -__builtin_inff());
+            }
         }
     }
 }
@@ -519,11 +598,21 @@ extern "C" int bpe_adjust_logits(const void *logits, int64_t logits_stride, int 
     p.out_stride = out_stride;
     p.rows = (int32_t)rows;
     p.n_vocab = (int32_t)n_vocab;
-    const dim3 grid((unsigned)((n_vocab + kSlice - 1) / kSlice), (unsigned)std::min<int64_t>(rows, 32768));
-    void (*kernel)(AdjustParams) = dtype == BPE_F32 ? adjust_kernel<F32, F32>
-                                   : dtype == BPE_BF16 ? (out_dtype == BPE_F32 ? adjust_kernel<Bf16, F32> : adjust_kernel<Bf16, Bf16>)
-                                                       : (out_dtype == BPE_F32 ? adjust_kernel<F16, F32> : adjust_kernel<F16, F16>);
-    return launch(kernel, grid, kGroupThreads, p, stream, "bpe_adjust_logits launch");
+    const bool lists = p.rules.n_history > 0 || p.rules.n_bias > 0;
+    // Four workgroups per compute unit if the slices can be as short as 2,048 tokens.
+    const int64_t per_row = std::max<int64_t>(1024 / rows, (n_vocab + kAdjustSlice - 1) / kAdjustSlice);
+    p.slice = (int32_t)std::max<int64_t>(((n_vocab + per_row - 1) / per_row + 31) & ~31ll, 2048);
+    p.slices = (int32_t)((n_vocab + p.slice - 1) / p.slice);
+    if (rows * p.slices > 0x7FFFFFFF) { set_error("bpe_adjust_logits: rows %lld and n_vocab %lld are too large together", (long long)rows, (long long)n_vocab); return BPE_ERR_SIZE; }
+    void (*kernel)(AdjustParams) = nullptr;
+#define ADJUST(IN, OUT) kernel = lists ? adjust_kernel<IN, OUT, true> : adjust_kernel<IN, OUT, false>
+    if (dtype == BPE_F32) ADJUST(F32, F32);
+    else if (dtype == BPE_BF16 && out_dtype == BPE_F32) ADJUST(Bf16, F32);
+    else if (dtype == BPE_BF16) ADJUST(Bf16, Bf16);
+    else if (out_dtype == BPE_F32) ADJUST(F16, F32);
+    else ADJUST(F16, F16);
+#undef ADJUST
+    return launch(kernel, dim3((unsigned)(rows * p.slices)), kAdjustThreads, p, stream, "bpe_adjust_logits launch");
 }
 
 static int check_top(int64_t rows, int64_t n_vocab, int64_t k) {
