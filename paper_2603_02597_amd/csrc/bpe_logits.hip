@@ -36,7 +36,7 @@ __device__ __forceinline__ const uint32_t *row_mask(const bpe_logit_rules &r, in
 // A workgroup takes a slice of a row.  With LISTS it first counts the row's history in LDS and marks the biased tokens, then makes one
 // pass over the slice, sixteen bytes per lane; the biased tokens, which that pass leaves out, come last.  Every slice of a row
 // reads the row's whole history: slices are as long as LDS allows with two workgroups per compute unit.
-constexpr int kAdjustThreads = 512, kAdjustSlice = 16384;
+constexpr int kAdjustThreads = 1024, kAdjustSlice = 16384;
 constexpr uint32_t kBiased = 0x80000000u;             // in a count
 template <class IN, class OUT, bool LISTS>
 __global__ void __launch_bounds__(kAdjustThreads) adjust_kernel(AdjustParams p) {
@@ -71,6 +71,13 @@ __global__ void __launch_bounds__(kAdjustThreads) adjust_kernel(AdjustParams p) 
             if (v >= first && v < last) atomicAdd(&count[v - first], 1u);
         };
         int i = begin + 4 * tid;
+        for (; i <= end - 4 - 12 * kAdjustThreads; i += 16 * kAdjustThreads) {
+            Int4Any v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = *(const Int4Any *)(r.history + i + q * 4 * kAdjustThreads);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) { note(v[q][0]); note(v[q][1]); note(v[q][2]); note(v[q][3]); }
+        }
         for (; i <= end - 4; i += 4 * kAdjustThreads) {
             const Int4Any v = *(const Int4Any *)(r.history + i);
             note(v[0]); note(v[1]); note(v[2]); note(v[3]);
