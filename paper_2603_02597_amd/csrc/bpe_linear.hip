@@ -187,12 +187,6 @@ __global__ void __launch_bounds__(kGroupThreads) linear_rows_kernel(LinearParams
     }
 }
 
-// What a wavefront's lanes have written to LDS is there for its other lanes.
-__device__ __forceinline__ void wave_sync() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 // More rows.  A workgroup makes BM x BN of out, WM x WN wavefronts side by side, 64 columns of k at a time through two buffers in LDS.
 typedef float F16v __attribute__((ext_vector_type(16)));
 // D = A B + C on 32 x 32 x 16: lane l gives A[l % 32][8 (l / 32) ..+7] and B[8 (l / 32) ..+7][l % 32] and holds

@@ -29,6 +29,12 @@ __device__ __forceinline__ float load_as_float(const void *p, int64_t i, int dty
     return dtype == BPE_BF16 ? to_float<Bf16>(v) : to_float<F16>(v);
 }
 
+// What a wavefront's lanes have written to LDS is there for its other lanes.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // One launch of a kernel whose only argument is its parameter block.
 template <class P>
 inline int launch(void (*kernel)(P), dim3 grid, int block, P &p, void *stream, const char *what) {
