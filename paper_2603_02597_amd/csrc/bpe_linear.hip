@@ -187,7 +187,7 @@ __global__ void __launch_bounds__(kGroupThreads) linear_rows_kernel(LinearParams
     }
 }
 
-// More rows.  A workgroup makes BM x BN of out, WM x WN wavefronts side by side, 64 columns of k at a time through two buffers in LDS.
+// More rows.  A workgroup makes BM x BN of out, WM x WN wavefronts side by side, 64 columns of k at a time through LDS.
 typedef float F16v __attribute__((ext_vector_type(16)));
 // D = A B + C on 32 x 32 x 16: lane l gives A[l % 32][8 (l / 32) ..+7] and B[8 (l / 32) ..+7][l % 32] and holds
 // C[e % 4 + 8 (e / 4) + 4 (l / 32)][l % 32] in element e.
@@ -204,9 +204,10 @@ template <> __device__ __forceinline__ F16v mma32<F16>(U4 a, U4 b, F16v c) {
 __device__ __forceinline__ void load_lds(uint32_t lds, const char *base, uint32_t offset) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
 }
-// This wavefront's loads have arrived and its reads of LDS are done; then the other wavefronts'.
-__device__ __forceinline__ void wait_and_meet() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+// All but this wavefront's last LATER loads have arrived and its reads of LDS are done; then the other wavefronts'.
+template <int LATER> __device__ __forceinline__ void wait_and_meet() {
+    static_assert(LATER < 64, "");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LATER) : "memory");
 }
 
 // Which tile of out a workgroup makes.  Workgroups go round the eight chiplets by their index, and each chiplet has an L2 of its
@@ -224,13 +225,13 @@ __device__ __forceinline__ bool tile_of(int64_t tiles_m, int64_t tiles_n, int sp
 }
 static int64_t tile_grid(int64_t tiles_m, int64_t tiles_n, int splits) { return (tiles_m * tiles_n * splits + 7) / 8 * 8; }
 
-template <class T, int BM, int BN, int WM, int WN, bool DIRECT>
+template <class T, int BM, int BN, int WM, int WN, int XS, bool DIRECT>
 __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParams p) {
     constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
     constexpr int kLoadsX = BM / 8 / NW, kLoadsW = BN / 8 / NW, kLoads = kLoadsX + kLoadsW;      // of eight rows of 64 columns
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "");
-    constexpr int kBlock = (BM + BN) * 128;
-    __shared__ __attribute__((aligned(1024))) char lds[2 * kBlock];
+    constexpr int kX = BM * 128, kW = BN * 128;                        // bytes of a block's rows of x and of weight: XS and two of them
+    __shared__ __attribute__((aligned(1024))) char lds[XS * kX + 2 * kW];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int64_t tile_m, tile_n;
     int split;
@@ -250,61 +251,82 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
     }
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wv * 1024;
     U4 held[DIRECT ? 1 : kLoads];      // rows at any alignment pass through registers
-    auto load_part = [&](int buf, int t, int q) {
+    // Load q of block t: of x into the slot at x_slot, or of weight at w_slot.
+    auto load_part = [&](int x_slot, int w_slot, int t, int q) {
         const char *base = (q < kLoadsX ? xb : wb) + 128 * (int64_t)t;
-        if constexpr (DIRECT) load_lds(lds_base + buf + q * (NW * 1024), base, at[q]);
+        if constexpr (DIRECT) load_lds(lds_base + (q < kLoadsX ? x_slot + q * (NW * 1024) : w_slot + (q - kLoadsX) * (NW * 1024)), base, at[q]);
         else held[q] = load16((const uint16_t *)(base + at[q]));
     };
-    auto store_part = [&](int buf, int q) {
-        if constexpr (!DIRECT) *(U4 *)(lds + buf + (q * NW + wv) * 1024 + 16 * lane) = held[q];
+    auto store_part = [&](int x_slot, int w_slot, int q) {
+        if constexpr (!DIRECT)
+            *(U4 *)(lds + (q < kLoadsX ? x_slot + q * (NW * 1024) : w_slot + (q - kLoadsX) * (NW * 1024)) + wv * 1024 + 16 * lane) = held[q];
     };
     const int wm = wv / WN, wn = wv % WN;
-    const int xrow = (wm * (BM / WM) + (lane & 31)) * 128, wrow = BM * 128 + (wn * (BN / WN) + (lane & 31)) * 128;
+    const int xrow = (wm * (BM / WM) + (lane & 31)) * 128, wrow = (wn * (BN / WN) + (lane & 31)) * 128;
     const int first = ((lane >> 5) ^ (lane & 7)) * 16;
     F16v acc[TM][TN] = {};
     U4 frag[2][2][TM + TN];            // [half of a block][step of 16 columns][rows of x, rows of weight]
-    auto read_part = [&](int buf, int half, int q) {
+    auto read_part = [&](int x_slot, int w_slot, int half, int q) {
         const int s = q / (TM + TN), f = q % (TM + TN), g = first ^ (32 * (2 * half + s));
-        frag[half][s][f] = *(const U4 *)(lds + (buf + (f < TM ? xrow : wrow) + g) + (f < TM ? f : f - TM) * 4096);
+        frag[half][s][f] = *(const U4 *)(lds + ((f < TM ? x_slot + xrow : w_slot + wrow) + g) + (f < TM ? f : f - TM) * 4096);
     };
     constexpr int kReads = 2 * (TM + TN), kProducts = 2 * TM * TN;
-    // The products of one half of a block, with the reads of the other half (of the block in `reads`) spread among them, and in the
-    // second half the loads of a later block (what went into registers goes on to `loads` in the first half after).
-    auto phase = [&](auto which, int reads, int loads, int t_load) {
-        constexpr int half = decltype(which)::value;
+    // The products of one half of a block, and spread among them: the reads of the other half (of the block in the slots xr, wr), the
+    // loads [L0, L1) of block t_load into xl, wl, and the stores [S0, S1) to xs, ws of what passes through registers.
+    auto phase = [&](auto which, auto l0, auto l1, auto s0, auto s1, int xr, int wr, int xl, int wl, int t_load, int xs, int ws) {
+        constexpr int half = decltype(which)::value, L0 = decltype(l0)::value, L = decltype(l1)::value - L0, S0 = decltype(s0)::value, S = decltype(s1)::value - S0;
 #pragma unroll
         for (int q = 0; q < kProducts; ++q) {
 #pragma unroll
-            for (int r = q * kReads / kProducts; r < (q + 1) * kReads / kProducts; ++r) read_part(reads, half ^ 1, r);
+            for (int r = q * kReads / kProducts; r < (q + 1) * kReads / kProducts; ++r) read_part(xr, wr, half ^ 1, r);
 #pragma unroll
-            for (int l = q * kLoads / kProducts; l < (q + 1) * kLoads / kProducts; ++l) {
-                if constexpr (half == 1) load_part(loads, t_load, l);
-                else store_part(loads, l);
-            }
+            for (int l = L0 + q * L / kProducts; l < L0 + (q + 1) * L / kProducts; ++l) load_part(xl, wl, t_load, l);
+#pragma unroll
+            for (int l = S0 + q * S / kProducts; l < S0 + (q + 1) * S / kProducts; ++l) store_part(xs, ws, l);
             const int s = q / (TM * TN), a = q / TN % TM, b = q % TN;
             acc[a][b] = mma32<T>(frag[half][s][TM + b], frag[half][s][a], acc[a][b]);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    constexpr std::integral_constant<int, 0> none;
+    constexpr std::integral_constant<int, 1> second;
+    constexpr std::integral_constant<int, kLoadsX> x_end;
+    constexpr std::integral_constant<int, kLoads> all;
     if (blocks > 0) {
+        // Slots of block t: x in t % XS, weight in t % 2.  A block's slots are free when the middle of it is reached, where its second
+        // half has been read; from there on weight of block t + 2 is loaded, and x too.  With a third slot x of block t + 2 is loaded
+        // in the first half of block t already: loads then come evenly, and may take longer.
+        constexpr bool kThird = XS == 3;
+        int x0 = 0, x1 = kX, x2 = XS == 3 ? 2 * kX : 0, w0 = XS * kX, w1 = w0 + kW;       // of blocks t, t + 1, t + 2
 #pragma unroll
-        for (int q = 0; q < kLoads; ++q) load_part(0, 0, q);
+        for (int q = 0; q < kLoads; ++q) load_part(x0, w0, 0, q);
 #pragma unroll
-        for (int q = 0; q < kLoads; ++q) store_part(0, q);
-        wait_and_meet();
+        for (int q = 0; q < kLoads; ++q) store_part(x0, w0, q);
+        wait_and_meet<0>();
 #pragma unroll
-        for (int q = 0; q < kReads; ++q) read_part(0, 0, q);
+        for (int q = 0; q < kReads; ++q) read_part(x0, w0, 0, q);
 #pragma unroll
-        for (int q = 0; q < kLoads; ++q) load_part(kBlock, min(1, blocks - 1), q);
-        int mine = 0;
-        for (int t = 0; t < blocks; ++t) {
-            phase(std::integral_constant<int, 0>(), mine, mine ^ kBlock, 0);
-            wait_and_meet();             // block t + 1 is there, and nobody reads block t any more
-            // (behind the last block but one: that block again, for nobody)
-            phase(std::integral_constant<int, 1>(), mine ^ kBlock, mine, min(t + 2, blocks - 1));
-            mine ^= kBlock;
+        for (int q = 0; q < kLoads; ++q) load_part(x1, w1, min(1, blocks - 1), q);
+        if constexpr (kThird) {
+#pragma unroll
+            for (int q = 0; q < kLoadsX; ++q) store_part(x1, w1, q);
         }
-        wait_and_meet();
+        for (int t = 0; t < blocks; ++t) {
+            // (behind the last block: that block again, for nobody)
+            const int t2 = min(t + 2, blocks - 1);
+            if constexpr (kThird) phase(none, none, x_end, x_end, all, x0, w0, x2, 0, t2, 0, w1);
+            else phase(none, none, none, none, all, x0, w0, 0, 0, 0, x1, w1);
+            wait_and_meet<kThird && DIRECT ? kLoadsX : 0>();          // block t + 1 is there, and nobody reads block t any more
+            if constexpr (kThird) phase(second, x_end, all, none, x_end, x1, w1, 0, w0, t2, x2, 0);
+            else phase(second, none, all, none, none, x1, w1, x0, w0, t2, 0, 0);
+            const int x = x0, w = w0;
+            x0 = x1;
+            x1 = kThird ? x2 : x;
+            x2 = x;
+            w0 = w1;
+            w1 = w;
+        }
+        wait_and_meet<0>();
     }
     // The columns behind the last whole block, filled up with zeros.
     if (split == p.splits - 1 && (p.k & 63)) {
@@ -312,13 +334,13 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
         for (int q = 0; q < kLoads; ++q) {
             const int row = ((q < kLoadsX ? q : q - kLoadsX) * NW + wv) * 8 + row8;
             const uint16_t *from = q < kLoadsX ? p.x + min(i0 + row, p.m - 1) * p.x_stride : p.w + min(j0 + row, p.n - 1) * p.w_stride;
-            *(U4 *)(lds + (q * NW + wv) * 1024 + 16 * lane) = load_tail(from, 64 * all_blocks + 8 * group, p.k);
+            *(U4 *)(lds + (q < kLoadsX ? q * NW * 1024 : kX + (q - kLoadsX) * NW * 1024) + wv * 1024 + 16 * lane) = load_tail(from, 64 * all_blocks + 8 * group, p.k);
         }
         __syncthreads();
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
 #pragma unroll
-            for (int q = 0; q < kReads; ++q) read_part(0, half, q);
+            for (int q = 0; q < kReads; ++q) read_part(0, kX, half, q);
 #pragma unroll
             for (int q = 0; q < kProducts; ++q) {
                 const int s = q / (TM * TN), a = q / TN % TM, b = q % TN;
@@ -330,7 +352,7 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
     // The result goes through LDS, 32 rows of a wavefront's part at a time, so that a row's columns leave next to each other:
     // the lanes hold one row each, four columns at a time.  (The padding of four columns spreads the rows over the banks.)
     constexpr int kCols = 32 * TN, kPitch = kCols + 4, kLanesPerRow = kCols / 4;
-    static_assert(NW * 32 * kPitch * 4 <= 2 * kBlock, "the rows of all wavefronts fit the buffers");
+    static_assert(NW * 32 * kPitch * 4 <= XS * kX + 2 * kW, "the rows of all wavefronts fit the buffers");
     float *stage = (float *)lds + wv * (32 * kPitch);
 #pragma unroll
     for (int a = 0; a < TM; ++a) {
@@ -453,18 +475,18 @@ static int launch_linear(LinearParams &p, void *workspace, void *stream) {
     p.part_stride = (int32_t)part_stride_of(p.n);
     const bool direct = p.x_stride % 8 == 0 && p.w_stride % 8 == 0 && !(((uintptr_t)p.x | (uintptr_t)p.w) & 15);
     void (*kernel)(LinearParams) = nullptr;
-#define TILE(INDEX, BM, BN, WM, WN) \
+#define TILE(INDEX, BM, BN, WM, WN, XS) \
     case INDEX: \
         static_assert(kLinearTiles[INDEX].bm == BM && kLinearTiles[INDEX].bn == BN, ""); \
-        kernel = direct ? linear_block_kernel<T, BM, BN, WM, WN, true> : linear_block_kernel<T, BM, BN, WM, WN, false>; \
+        kernel = direct ? linear_block_kernel<T, BM, BN, WM, WN, XS, true> : linear_block_kernel<T, BM, BN, WM, WN, XS, false>; \
         break
     switch (plan.tile) {
-        TILE(0, 32, 128, 1, 4);
-        TILE(1, 32, 256, 1, 4);
-        TILE(2, 64, 128, 1, 4);
-        TILE(3, 64, 256, 1, 4);
-        TILE(4, 128, 128, 2, 2);
-        TILE(5, 256, 256, 2, 2);
+        TILE(0, 32, 128, 1, 4, 2);
+        TILE(1, 32, 256, 1, 4, 2);
+        TILE(2, 64, 128, 1, 4, 2);
+        TILE(3, 64, 256, 1, 4, 2);
+        TILE(4, 128, 128, 2, 2, 3);
+        TILE(5, 256, 256, 2, 2, 3);
     }
 #undef TILE
     const int rc = launch(kernel, dim3((unsigned)grid), kGroupThreads, p, stream, what);
