@@ -49,50 +49,73 @@ __device__ __forceinline__ float activate(float v, int activation) {
 typedef float F4Any __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint16_t H4Any __attribute__((ext_vector_type(4), aligned(2)));
 
-__device__ __forceinline__ float finish(const LinearParams &p, float v, float bias, float residual) {
-    return activate(v + bias, p.activation) + residual;
+__device__ __forceinline__ float out_to_float(const LinearParams &p, uint16_t v) { return p.out_dtype == BPE_BF16 ? to_float<Bf16>(v) : to_float<F16>(v); }
+__device__ __forceinline__ uint16_t out_from_float(const LinearParams &p, float v) { return p.out_dtype == BPE_BF16 ? from_float<Bf16>(v) : from_float<F16>(v); }
+__device__ __forceinline__ F4 bias_of(const LinearParams &p, int j) {          // of columns j .. j + 3, which exist
+    if (!p.bias) return F4{0, 0, 0, 0};
+    if (p.bias_dtype == BPE_F32) return *(const F4Any *)((const float *)p.bias + j);
+    const H4Any b = *(const H4Any *)((const uint16_t *)p.bias + j);
+    F4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = p.bias_dtype == BPE_BF16 ? to_float<Bf16>(b[e]) : to_float<F16>(b[e]);
+    return v;
 }
-// The epilogue of columns j .. j + 3 of row i, as far as they exist.  (Every lane of a call takes the same branches but the last.)
-__device__ __forceinline__ void put4(const LinearParams &p, int i, int j, F4 v) {
-    const int64_t at = i * p.out_stride + j, from = i * p.residual_stride + j;
+// The epilogue of columns j .. j + 3, as far as they exist, of ROWS rows that are `step` apart, as far as they do.  ACTIVATED: with any
+// activation; else without one.  (Every lane of a call takes the same branches but those at the edges.)
+template <int ROWS, bool ACTIVATED>
+__device__ __forceinline__ void put(const LinearParams &p, int i, int step, int j, F4 (&v)[ROWS]) {
     if (j + 3 >= p.n) {
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) {
 #pragma unroll 1
-        for (int e = 0; e < 4 && j + e < p.n; ++e) {
-            const float x = e == 0 ? v[0] : e == 1 ? v[1] : e == 2 ? v[2] : v[3];
-            const float o = finish(p, x, p.bias ? load_as_float(p.bias, j + e, p.bias_dtype) : 0.0f,
-                                   p.residual ? load_as_float(p.residual, from + e, p.out_dtype) : 0.0f);
-            if (p.out_dtype == BPE_F32) ((float *)p.out)[at + e] = o;
-            else ((uint16_t *)p.out)[at + e] = p.out_dtype == BPE_BF16 ? from_float<Bf16>(o) : from_float<F16>(o);
+            for (int e = 0; e < 4; ++e) {
+                if (i + u * step >= p.m || j + e >= p.n) break;
+                const int64_t row = i + u * step;
+                float x = e == 0 ? v[u][0] : e == 1 ? v[u][1] : e == 2 ? v[u][2] : v[u][3];
+                if (p.bias) x += load_as_float(p.bias, j + e, p.bias_dtype);
+                if (ACTIVATED) x = activate(x, p.activation);
+                if (p.residual) x += load_as_float(p.residual, row * p.residual_stride + j + e, p.out_dtype);
+                const int64_t at = row * p.out_stride + j + e;
+                if (p.out_dtype == BPE_F32) ((float *)p.out)[at] = x;
+                else ((uint16_t *)p.out)[at] = out_from_float(p, x);
+            }
         }
         return;
     }
     if (p.bias) {
-        if (p.bias_dtype == BPE_F32) {
-            v += *(const F4Any *)((const float *)p.bias + j);
-        } else {
-            const H4Any b = *(const H4Any *)((const uint16_t *)p.bias + j);
+        const F4 b = bias_of(p, j);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += p.bias_dtype == BPE_BF16 ? to_float<Bf16>(b[e]) : to_float<F16>(b[e]);
+        for (int u = 0; u < ROWS; ++u) v[u] += b;
+    }
+    if (ACTIVATED && p.activation != BPE_ACT_NONE) {
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[u][e] = activate(v[u][e], p.activation);
+    }
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u) {
+        const int64_t row = i + u * step, at = row * p.out_stride + j, from = row * p.residual_stride + j;
+        if (row >= p.m) break;
+        if (p.out_dtype == BPE_F32) {
+            if (p.residual) v[u] += *(const F4Any *)((const float *)p.residual + from);
+            *(F4Any *)((float *)p.out + at) = v[u];
+        } else {
+            H4Any o;
+            if (p.residual) {
+                o = *(const H4Any *)((const uint16_t *)p.residual + from);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[u][e] += out_to_float(p, o[e]);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = out_from_float(p, v[u][e]);
+            *(H4Any *)((uint16_t *)p.out + at) = o;
         }
     }
-    if (p.activation != BPE_ACT_NONE) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = activate(v[e], p.activation);
-    }
-    if (p.out_dtype == BPE_F32) {
-        if (p.residual) v += *(const F4Any *)((const float *)p.residual + from);
-        *(F4Any *)((float *)p.out + at) = v;
-        return;
-    }
-    H4Any o;
-    if (p.residual) {
-        o = *(const H4Any *)((const uint16_t *)p.residual + from);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += p.out_dtype == BPE_BF16 ? to_float<Bf16>(o[e]) : to_float<F16>(o[e]);
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = p.out_dtype == BPE_BF16 ? from_float<Bf16>(v[e]) : from_float<F16>(v[e]);
-    *(H4Any *)((uint16_t *)p.out + at) = o;
+}
+__device__ __forceinline__ void put4(const LinearParams &p, int i, int j, F4 v) {
+    F4 one[1] = {v};
+    put<1, true>(p, i, 1, j, one);
 }
 
 // Sixteen bytes at any even address: the hardware asks for no more.
@@ -363,15 +386,29 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
                 *(F4 *)(stage + (lane & 31) * kPitch + 32 * b + 8 * e + 4 * (lane >> 5)) =
                     F4{acc[a][b][4 * e], acc[a][b][4 * e + 1], acc[a][b][4 * e + 2], acc[a][b][4 * e + 3]};
         wave_sync();
-        const int j = j0 + wn * kCols + 4 * (lane % kLanesPerRow);
+        // a batch of rows at a time: their reads and their stores are under way together
+        constexpr int kStep = 64 / kLanesPerRow, kBatch = 32 / kStep < 8 ? 32 / kStep : 8;
+        const int j = j0 + wn * kCols + 4 * (lane % kLanesPerRow), i = i0 + wm * (BM / WM) + 32 * a + lane / kLanesPerRow;
+        const float *mine = stage + lane / kLanesPerRow * kPitch + 4 * (lane % kLanesPerRow);
+        if (p.splits > 1 || p.activation == BPE_ACT_NONE) {
 #pragma unroll 1
-        for (int r = lane / kLanesPerRow; r < 32; r += 64 / kLanesPerRow) {
-            const F4 v = *(const F4 *)(stage + r * kPitch + 4 * (lane % kLanesPerRow));
-            const int i = i0 + wm * (BM / WM) + 32 * a + r;
-            if (i < p.m && j < p.n) {
-                if (p.splits > 1) *(F4 *)(p.part + ((int64_t)split * p.m + i) * p.part_stride + j) = v;
-                else put4(p, i, j, v);
+            for (int r = 0; r < 32; r += kBatch * kStep) {
+                F4 v[kBatch];
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) v[u] = *(const F4 *)(mine + (r + u * kStep) * kPitch);
+                if (j >= p.n) continue;
+                if (p.splits > 1) {
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u)
+                        if (i + r + u * kStep < p.m) *(F4 *)(p.part + ((int64_t)split * p.m + i + r + u * kStep) * p.part_stride + j) = v[u];
+                } else {
+                    put<kBatch, false>(p, i + r, kStep, j, v);
+                }
             }
+        } else if (j < p.n) {
+#pragma unroll 1
+            for (int r = 0; r < 32; r += kStep)
+                if (i + r < p.m) put4(p, i + r, j, *(const F4 *)(mine + r * kPitch));
         }
         wave_sync();
     }
