@@ -41,7 +41,7 @@ __device__ __forceinline__ float activate(float v, int activation) {
         case BPE_ACT_RELU: return v > 0.0f ? v : (v != v ? v : 0.0f);
         case BPE_ACT_GELU: return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
         case BPE_ACT_GELU_TANH: return 0.5f * v * (1.0f + tanhf(0.79788456080286536f * (v + 0.044715f * v * v * v)));
-        case BPE_ACT_SILU: return v / (1.0f + __expf(-v));
+        case BPE_ACT_SILU: return v / (1.0f + expf(-v));
         default: return v;
     }
 }
@@ -122,92 +122,82 @@ __device__ __forceinline__ void put4(const LinearParams &p, int i, int j, F4 v) 
 typedef uint32_t U4Any __attribute__((ext_vector_type(4), aligned(2)));
 __device__ __forceinline__ U4 load16(const uint16_t *at) { return *(const U4Any *)at; }
 
-// Eight elements of a row from column t on, zeros behind the row's end.
+// Eight elements of a row from column t on, zeros behind the row's end: the row's last eight at most, shifted.  No branch for k >= 8.
 __device__ __forceinline__ U4 load_tail(const uint16_t *row, int t, int k) {
-    if (t + 8 <= k) return load16(row + t);
-    H8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (k < 8) {
+        H8 v = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (t + e < k) v[e] = row[t + e];
-    return __builtin_bit_cast(U4, v);
+        for (int e = 0; e < 8; ++e)
+            if (t + e < k) v[e] = row[t + e];
+        return __builtin_bit_cast(U4, v);
+    }
+    const int over = max(t - (k - 8), 0);                 // elements of the eight that lie behind the end
+    typedef uint64_t Two __attribute__((ext_vector_type(2)));
+    const Two v = __builtin_bit_cast(Two, load16(row + (t - over)));
+    const uint32_t shift = 16u * (uint32_t)(over & 3);
+    const uint64_t low = over < 4 ? v[0] : v[1], high = over < 4 ? v[1] : 0;
+    Two o = {low >> shift | (shift ? high << (64 - shift) : 0), high >> shift};
+    if (over >= 8) o = Two{0, 0};
+    return __builtin_bit_cast(U4, o);
 }
 
-// Up to 64 rows of x: the call is as long as reading weight takes, so weight goes from memory straight into the matrix
-// cores' registers and every byte of it is asked for once.  A workgroup takes 16 NT rows of weight, its four wavefronts a
-// quarter of k each (a long row is 4 streams, and a vocabulary of few rows still fills the chip); their sums meet in LDS.
-// weight is the left operand: a lane ends with four neighbouring columns of one row of out.
-// A step is 64 columns, whole lines of memory: two products, whose loads lie next to each other.
-template <class T, int MT, int NT, int AHEAD>
+// A few rows of x: the call is as long as reading weight takes, so weight goes from memory straight into the matrix cores'
+// registers.  A workgroup takes 16 rows of weight, its four wavefronts a quarter of k each (so a vocabulary of few rows still fills
+// the chip); their sums meet in LDS.  A step is 64 columns, whole lines of memory, and four steps are under way at a time.
+// weight is the left operand: a lane ends with four neighbouring columns of one row of out; rows behind the last of x repeat it and
+// are dropped.  Bound by memory: 1 x 50256 x 1024 18 us, 1 x 100256 x 4096 143 us, 5.7 TB/s; 1 x 2048 x 2048 7 us, of which 5 are the launch.
+constexpr int kRowsAhead = 4;
+template <class T>
 __global__ void __launch_bounds__(kGroupThreads) linear_rows_kernel(LinearParams p) {
-    __shared__ F4 part[kWavesPerGroup][MT * NT][kWave];
+    __shared__ F4 part[kWavesPerGroup][kWave];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int j0 = blockIdx.x * (16 * NT);
+    const int j0 = blockIdx.x * 16, group = 8 * (lane >> 4);
     const int steps = p.k >> 6, from = (int)((int64_t)steps * wv / kWavesPerGroup), to = (int)((int64_t)steps * (wv + 1) / kWavesPerGroup);
-    const uint16_t *w[NT], *x[MT];
-#pragma unroll
-    for (int b = 0; b < NT; ++b) w[b] = p.w + min(j0 + 16 * b + (lane & 15), p.n - 1) * p.w_stride + 8 * (lane >> 4);
-#pragma unroll
-    for (int a = 0; a < MT; ++a) x[a] = p.x + min(16 * a + (lane & 15), p.m - 1) * p.x_stride + 8 * (lane >> 4);
-    F4 acc[MT][NT] = {};
-    U4 wf[AHEAD][NT][2], xf[AHEAD][MT][2];
+    const uint16_t *w = p.w + min(j0 + (lane & 15), p.n - 1) * p.w_stride, *x = p.x + min(lane & 15, p.m - 1) * p.x_stride;
+    F4 acc = {0, 0, 0, 0};
+    U4 wf[kRowsAhead][2], xf[kRowsAhead][2];
     auto load = [&](int u, int step) {
 #pragma unroll
-        for (int b = 0; b < NT; ++b)
+        for (int h = 0; h < 2; ++h) wf[u][h] = load16(w + 64 * (int64_t)step + 32 * h + group);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) wf[u][b][h] = load16(w[b] + 64 * (int64_t)step + 32 * h);
-#pragma unroll
-        for (int a = 0; a < MT; ++a)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) xf[u][a][h] = load16(x[a] + 64 * (int64_t)step + 32 * h);
+        for (int h = 0; h < 2; ++h) xf[u][h] = load16(x + 64 * (int64_t)step + 32 * h + group);
     };
     auto multiply = [&](int u) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int a = 0; a < MT; ++a)
-#pragma unroll
-                for (int b = 0; b < NT; ++b) acc[a][b] = mma16<T>(wf[u][b][h], xf[u][a][h], acc[a][b]);
+        for (int h = 0; h < 2; ++h) acc = mma16<T>(wf[u][h], xf[u][h], acc);
     };
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
+    for (int u = 0; u < kRowsAhead; ++u)
         if (from + u < to) load(u, from + u);
     int step = from;
-    for (; step + 2 * AHEAD <= to; step += AHEAD)
+    for (; step + 2 * kRowsAhead <= to; step += kRowsAhead)
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
+        for (int u = 0; u < kRowsAhead; ++u) {
             multiply(u);
-            load(u, step + AHEAD + u);
+            load(u, step + kRowsAhead + u);
         }
-    for (; step < to; step += AHEAD)
+    for (; step < to; step += kRowsAhead)
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
+        for (int u = 0; u < kRowsAhead; ++u)
             if (step + u < to) {
                 multiply(u);
-                if (step + AHEAD + u < to) load(u, step + AHEAD + u);
+                if (step + kRowsAhead + u < to) load(u, step + kRowsAhead + u);
             }
     if (wv == kWavesPerGroup - 1 && (p.k & 63)) {
-        const int t = (p.k & ~63) + 8 * (lane >> 4);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int b = 0; b < NT; ++b) wf[0][b][h] = load_tail(w[b] - 8 * (lane >> 4), t + 32 * h, p.k);
-#pragma unroll
-            for (int a = 0; a < MT; ++a) xf[0][a][h] = load_tail(x[a] - 8 * (lane >> 4), t + 32 * h, p.k);
+            wf[0][h] = load_tail(w, (p.k & ~63) + 32 * h + group, p.k);
+            xf[0][h] = load_tail(x, (p.k & ~63) + 32 * h + group, p.k);
         }
         multiply(0);
     }
-#pragma unroll
-    for (int a = 0; a < MT; ++a)
-#pragma unroll
-        for (int b = 0; b < NT; ++b) part[wv][a * NT + b][lane] = acc[a][b];
+    part[wv][lane] = acc;
     __syncthreads();
-    for (int q = wv; q < MT * NT; q += kWavesPerGroup) {
-        F4 v = part[0][q][lane];
+    if (wv != 0) return;
 #pragma unroll
-        for (int s = 1; s < kWavesPerGroup; ++s) v += part[s][q][lane];
-        const int i = 16 * (q / NT) + (lane & 15), j = j0 + 16 * (q % NT) + 4 * (lane >> 4);
-        if (i < p.m && j < p.n) put4(p, i, j, v);
-    }
+    for (int s = 1; s < kWavesPerGroup; ++s) acc += part[s][lane];
+    const int i = lane & 15, j = j0 + 4 * (lane >> 4);
+    if (i < p.m && j < p.n) put4(p, i, j, acc);
 }
 
 // More rows.  A workgroup makes BM x BN of out, WM x WN wavefronts side by side, 64 columns of k at a time through LDS.
@@ -353,12 +343,16 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
     }
     // The columns behind the last whole block, filled up with zeros.
     if (split == p.splits - 1 && (p.k & 63)) {
-#pragma unroll 1
+        U4 last[kLoads];
+#pragma unroll
         for (int q = 0; q < kLoads; ++q) {
             const int row = ((q < kLoadsX ? q : q - kLoadsX) * NW + wv) * 8 + row8;
             const uint16_t *from = q < kLoadsX ? p.x + min(i0 + row, p.m - 1) * p.x_stride : p.w + min(j0 + row, p.n - 1) * p.w_stride;
-            *(U4 *)(lds + (q < kLoadsX ? q * NW * 1024 : kX + (q - kLoadsX) * NW * 1024) + wv * 1024 + 16 * lane) = load_tail(from, 64 * all_blocks + 8 * group, p.k);
+            last[q] = load_tail(from, 64 * all_blocks + 8 * group, p.k);
         }
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q)
+            *(U4 *)(lds + (q < kLoadsX ? q * NW * 1024 : kX + (q - kLoadsX) * NW * 1024) + wv * 1024 + 16 * lane) = last[q];
         __syncthreads();
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -500,7 +494,10 @@ static int launch_linear(LinearParams &p, void *workspace, void *stream) {
     const char *what = "bpe_linear launch";
     LinearPlan plan = plan_linear(p.m, p.n, p.k);
     p.splits = 1;
-    if (plan.tile < 0) return launch(linear_rows_kernel<T, 1, 1, 4>, dim3((unsigned)(((int64_t)p.n + 15) / 16)), kGroupThreads, p, stream, what);
+    const bool direct = p.x_stride % 8 == 0 && p.w_stride % 8 == 0 && !(((uintptr_t)p.x | (uintptr_t)p.w) & 15);
+    // (rows at odd addresses cost linear_rows_kernel more than they cost a tile: 1 x 50256 x 1023 48 us and in tiles 34)
+    if (plan.tile < 0 && !direct && (int64_t)p.n * p.k > (1 << 24)) plan = {0, 1};
+    if (plan.tile < 0) return launch(linear_rows_kernel<T>, dim3((unsigned)(((int64_t)p.n + 15) / 16)), kGroupThreads, p, stream, what);
     // A tile's rows are addressed by 32-bit offsets; rows that lie further apart take the simple kernel.
     const bool far = p.x_stride >= (1 << 21) || p.w_stride >= (1 << 21);
     const int64_t bm = far ? 64 : kLinearTiles[plan.tile].bm, bn = far ? 64 : kLinearTiles[plan.tile].bn;
@@ -510,7 +507,6 @@ static int launch_linear(LinearParams &p, void *workspace, void *stream) {
     if (far) return launch(linear_tile_kernel<T>, dim3((unsigned)grid), kGroupThreads, p, stream, what);
     p.part = (float *)workspace;
     p.part_stride = (int32_t)part_stride_of(p.n);
-    const bool direct = p.x_stride % 8 == 0 && p.w_stride % 8 == 0 && !(((uintptr_t)p.x | (uintptr_t)p.w) & 15);
     void (*kernel)(LinearParams) = nullptr;
 #define TILE(INDEX, BM, BN, WM, WN, XS) \
     case INDEX: \
