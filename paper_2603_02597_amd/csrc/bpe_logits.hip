@@ -165,17 +165,17 @@ __global__ void __launch_bounds__(kAdjustThreads) adjust_kernel(AdjustParams p) 
 
 // ---------------------------------------------------------------------------
 // The best tokens of a row, in one pass over it.  A workgroup goes through its part of a row and keeps, in LDS, every logit that
-// may still be among the k best: those not below a bound that at least k logits reach.  The bound is cheap: the threads are put
-// into 2^j >= k sets, and the least of the sets' largest logits so far is reached by one logit of every set.  (Of 8,192 random
-// logits it lets k ln k through, of later ones fewer and fewer.)  What was kept is cut down to the k best by histograms over the
-// range of what is left, and put in order by counting.  Logits are compared as (value, index from behind) in one 64-bit word, so no
-// two are equal and the order in which lanes append does not matter.
+// may still be among the k best: those not below a bound that at least k logits reach.  The bound is cheap: the k-th largest of the
+// threads' largest logits so far.  (Of 8,192 random logits it lets 73 through for k = 64, of later ones fewer and fewer.)  What was
+// kept is cut down to the k best by histograms over the range of what is left, and put in order by counting.  Logits are compared as
+// (value, index from behind) in one 64-bit word, so no two are equal and the order in which lanes append does not matter.
 constexpr int kTopThreads = 256, kTopWaves = kTopThreads / kWave;
 constexpr int kTopKeep = 4096;               // words in LDS: four workgroups per compute unit
 constexpr int kTopVectors = 4;               // sixteen-byte loads of a thread that are under way together
 constexpr int kTopBins = 1024;
 constexpr int kTopRank = 256;                // up to so many words are put in order by counting
 constexpr int kMaxTop = 256;
+constexpr float kLowest = -3.402823466e38f;       // of the finite floats
 constexpr float kLog2E = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // What a part leaves: its largest logit, the sum of exp(logit - largest), a bound that k of its words reach, the number of its words.
@@ -184,7 +184,7 @@ struct TopPart { float largest, sum, bound; int32_t words; };
 struct TopParams {
     const void *logits;
     int64_t logits_stride;
-    int32_t rows, n_vocab, k, sets;          // sets: power of two, k <= sets <= kTopThreads
+    int32_t rows, n_vocab, k;
     int32_t parts, part_len, part_keep;      // a row is cut into so many parts of part_len logits, each leaves up to part_keep words
     int32_t *ids;
     float *logprobs, *lse;
@@ -205,7 +205,7 @@ __device__ __forceinline__ uint64_t top_word(float x, int v) { return (uint64_t)
 
 struct TopShared {
     uint64_t word[kTopKeep];
-    uint32_t bin[kTopBins];
+    uint32_t bin[kTopBins];                  // (also the threads' largest logits)
     uint64_t few[kTopRank];
     float wave_value[kTopWaves];
     float2 wave_sum[kTopWaves];
@@ -220,6 +220,7 @@ __device__ __forceinline__ uint64_t bound_of_best(TopShared &sh, int count, int 
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     if (count <= kTopRank) return 0;
     int above = 0;                            // words above `high`: fewer than k
+    __syncthreads();                          // the bins may hold the threads' largest logits, which somebody still reads
     for (;;) {
         const int shift = max(0, 54 - __builtin_clzll((high - low) | 1));        // (high - low) >> shift < kTopBins
         for (int i = tid; i < kTopBins; i += kTopThreads) sh.bin[i] = 0;
@@ -320,23 +321,24 @@ template <class Op> __device__ __forceinline__ float wave_join(float v, Op op) {
     return join_groups<32>(v, op);
 }
 
-__device__ __forceinline__ float in_or_between(float a, float b, bool in_a_set) { return in_a_set ? fmaxf(a, b) : fminf(a, b); }
-// The least of the sets' largest values: reached by a logit of every set.  A set is `together` neighbouring threads, a power of two.
-__device__ __forceinline__ float least_of_sets(TopShared &sh, float largest, int sets) {
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    const int together = kTopThreads / sets;
-    float v = largest;
-    v = in_or_between(v, other_group<1>(v), 1 < together);
-    v = in_or_between(v, other_group<2>(v), 2 < together);
-    v = in_or_between(v, other_group<4>(v), 4 < together);
-    v = in_or_between(v, other_group<8>(v), 8 < together);
-    v = in_or_between(v, other_group<16>(v), 16 < together);
-    v = in_or_between(v, other_group<32>(v), 32 < together);
-    if (lane == 0) sh.wave_value[wv] = v;
+// A bound that the largest logits of k threads reach: their k-th largest, cut to the upper 16 bits of its place in the order.  Every
+// wavefront looks at all of them, four per lane, and finds the bound bit by bit.
+__device__ __forceinline__ float bound_of_threads(TopShared &sh, float largest, int k) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    sh.bin[tid] = order_key(largest);
     __syncthreads();
-    static_assert(kTopWaves == 4, "");
-    const float a = in_or_between(sh.wave_value[0], sh.wave_value[1], 64 < together), b = in_or_between(sh.wave_value[2], sh.wave_value[3], 64 < together);
-    return in_or_between(a, b, 128 < together);
+    static_assert(kTopThreads == 4 * kWave, "");
+    const U4 key = ((const U4 *)sh.bin)[lane];
+    uint32_t bound = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t at = bound | 1u << bit;
+        int reach = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) reach += __builtin_popcountll(__ballot(key[q] >= at));
+        bound = reach >= k ? at : bound;
+    }
+    return bound > order_key(-__builtin_inff()) ? key_value(bound) : kLowest;
 }
 
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
@@ -389,14 +391,14 @@ template <class IN>
 __global__ void __launch_bounds__(kTopThreads, 4) top_part_kernel(TopParams p) {
     constexpr int kPer = 16 / (int)sizeof(typename IN::raw), kRound = kTopThreads * kPer * kTopVectors;
     typedef typename IN::raw Vec __attribute__((ext_vector_type(kPer), aligned(sizeof(typename IN::raw))));
-    __shared__ TopShared sh;
+    __shared__ __attribute__((aligned(16))) TopShared sh;
     const int tid = threadIdx.x, lane = tid & 63;
     const int row = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
     const int first = part * p.part_len, last = min(first + p.part_len, p.n_vocab);
     const typename IN::raw *in = (const typename IN::raw *)p.logits + row * p.logits_stride;
     if (tid == 0) sh.n = 0;
     float largest = -__builtin_inff(), sum = 0.0f;
-    float bound = -3.402823466e38f;                       // logits below it are out; so is -infinity
+    float bound = kLowest;                                // logits below it are out; so is -infinity
     uint64_t bound_word = 0;                              // and words that are not above this one
     int before = 0, n_rounds = 0;
     for (int at = first; at < last; at += kRound, ++n_rounds) {
@@ -431,7 +433,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) top_part_kernel(TopParams p) {
             for (int e = 0; e < kPer; ++e) sum += exp_of(x[q][e] - ref);
         largest = m;
         const float bound_before = bound;                 // reached by k of the words that are there
-        if ((n_rounds & (n_rounds + 1)) == 0) bound = fmaxf(bound, least_of_sets(sh, largest, p.sets));   // rounds 0, 1, 3, 7, ...
+        if ((n_rounds & (n_rounds + 1)) == 0) bound = fmaxf(bound, bound_of_threads(sh, largest, p.k));   // rounds 0, 1, 3, 7, ...
         else __syncthreads();
         // A lane's logits that stay, one bit each: few, so they are read again.
         uint32_t stay = 0;
@@ -482,7 +484,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) top_part_kernel(TopParams p) {
     }
     __syncthreads();
     const float2 total = join_sums(sh, largest, sum);
-    if (n_rounds > 1) bound = fmaxf(bound, least_of_sets(sh, largest, p.sets));
+    if (n_rounds > 1) bound = fmaxf(bound, bound_of_threads(sh, largest, p.k));
     if (p.parts == 1) {
         write_row(p, sh, row, before, words_from(bound), total);
         return;
@@ -516,10 +518,10 @@ __global__ void __launch_bounds__(kTopThreads, 4) top_part_kernel(TopParams p) {
 
 // The best of the parts' best: none is below the highest of the parts' bounds.
 __global__ void __launch_bounds__(kTopThreads) top_join_kernel(TopParams p) {
-    __shared__ TopShared sh;
+    __shared__ __attribute__((aligned(16))) TopShared sh;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, row = blockIdx.x;
     const TopPart *left = p.left + (int64_t)row * p.parts;
-    float bound = -3.402823466e38f, largest = -__builtin_inff(), sum = 0.0f;
+    float bound = kLowest, largest = -__builtin_inff(), sum = 0.0f;
     for (int i = tid; i < p.parts; i += kTopThreads) {
         const TopPart t = left[i];
         const float m = fmaxf(largest, t.largest), ref = reference_of(m);
@@ -637,7 +639,7 @@ static int64_t top_parts(int64_t rows, int64_t n_vocab, int64_t k) {
     const int64_t parts = std::min(std::min(1024 / std::max<int64_t>(rows, 1), (n_vocab + 8191) / 8192), (int64_t)kTopKeep / k);
     return std::max<int64_t>(parts, 1);
 }
-// Words that a part leaves: k ln k of a part of one round are above its bound as a rule.
+// Words that a part leaves: a little more than k as a rule, for k = 256 (as many as there are threads) five times as many.
 static int64_t part_keep(int64_t parts, int64_t k) { return std::min<int64_t>(std::max<int64_t>(8 * k, 32), kTopKeep / parts); }
 
 extern "C" int64_t bpe_top_tokens_workspace_bytes(int64_t rows, int64_t n_vocab, int64_t k) {
@@ -669,7 +671,6 @@ extern "C" int bpe_top_tokens(const void *logits, int64_t logits_stride, int dty
     p.ids = ids;
     p.logprobs = logprobs;
     p.lse = lse;
-    for (p.sets = 1; p.sets < p.k;) p.sets *= 2;
     const int64_t parts = top_parts(rows, n_vocab, k);
     if (rows * parts > 0x7FFFFFFF) { set_error("bpe_top_tokens: rows out of range (%lld)", (long long)rows); return BPE_ERR_SIZE; }
     p.parts = (int32_t)parts;
