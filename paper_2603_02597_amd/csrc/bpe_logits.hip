@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(kAdjustThreads) adjust_kernel(AdjustParams p) 
 // (value, index from behind) in one 64-bit word, so no two are equal and the order in which lanes append does not matter.
 constexpr int kTopThreads = 256, kTopWaves = kTopThreads / kWave;
 constexpr int kTopKeep = 4096;               // words in LDS: four workgroups per compute unit
-constexpr int kTopVectors = 4;               // sixteen-byte loads of a thread that are under way together
+constexpr int kTopPerThread = 32;            // logits of a thread that are at hand together
 constexpr int kTopBins = 1024;
 constexpr int kTopRank = 256;                // up to so many words are put in order by counting
 constexpr int kMaxTop = 256;
@@ -389,7 +389,7 @@ __device__ __forceinline__ void write_row(const TopParams &p, TopShared &sh, int
 
 template <class IN>
 __global__ void __launch_bounds__(kTopThreads, 4) top_part_kernel(TopParams p) {
-    constexpr int kPer = 16 / (int)sizeof(typename IN::raw), kRound = kTopThreads * kPer * kTopVectors;
+    constexpr int kPer = 16 / (int)sizeof(typename IN::raw), kTopVectors = kTopPerThread / kPer, kRound = kTopThreads * kTopPerThread;
     typedef typename IN::raw Vec __attribute__((ext_vector_type(kPer), aligned(sizeof(typename IN::raw))));
     __shared__ __attribute__((aligned(16))) TopShared sh;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -469,7 +469,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) top_part_kernel(TopParams p) {
             count = left;
         };
         cut();
-        for (int bit = 0; bit < kTopVectors * kPer; ++bit) {
+        for (int bit = 0; bit < kTopPerThread; ++bit) {
             if (count > kTopKeep - kTopThreads) cut();
             if (stay >> bit & 1u) {
                 const uint64_t w = word_of(bit);
