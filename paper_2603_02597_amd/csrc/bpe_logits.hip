@@ -608,8 +608,9 @@ extern "C" int bpe_adjust_logits(const void *logits, int64_t logits_stride, int 
     p.rows = (int32_t)rows;
     p.n_vocab = (int32_t)n_vocab;
     const bool lists = p.rules.n_history > 0 || p.rules.n_bias > 0;
-    // Four workgroups per compute unit if the slices can be as short as 2,048 tokens.
-    const int64_t per_row = std::max<int64_t>(1024 / rows, (n_vocab + kAdjustSlice - 1) / kAdjustSlice);
+    // As many workgroups as are on the chip at once, if the slices can be as long: 64 rows of 100256 with lists 12.6 us, in twice as
+    // many slices 16.5.
+    const int64_t per_row = std::max<int64_t>(512 / rows, (n_vocab + kAdjustSlice - 1) / kAdjustSlice);
     p.slice = (int32_t)std::max<int64_t>(((n_vocab + per_row - 1) / per_row + 31) & ~31ll, 2048);
     p.slices = (int32_t)((n_vocab + p.slice - 1) / p.slice);
     if (rows * p.slices > 0x7FFFFFFF) { set_error("bpe_adjust_logits: rows %lld and n_vocab %lld are too large together", (long long)rows, (long long)n_vocab); return BPE_ERR_SIZE; }
