@@ -455,10 +455,13 @@ __global__ void __launch_bounds__(kGroupThreads) linear_join_kernel(LinearParams
 
 // Which tiles a product of these sizes takes, and into how many parts k is cut: what an estimate of the time says.  A tile's
 // row: its sides, how many of its workgroups a compute unit holds, us for a block of 64 columns when a workgroup waits for
-// its loads alone, and the TFLOP/s of the whole chip when nothing else bounds it.
-struct LinearTile { int bm, bn, resident; double block_us, tflops; };
+// its loads alone, us for its first loads and its result, and the TFLOP/s of the whole chip when nothing else bounds it.  The
+// numbers are fitted to the times of all tiles and parts on 93 sizes (m 5 to 8192, n 256 to 128000, k 64 to 4096); there the choice takes
+// 1.7 % longer than the best one on average, 23 % at worst.
+struct LinearTile { int bm, bn, resident; double block_us, tile_us, tflops; };
 constexpr LinearTile kLinearTiles[] = {
-    {32, 128, 4, 0.46, 556}, {32, 256, 2, 0.61, 590}, {64, 128, 3, 0.50, 795}, {64, 256, 2, 0.68, 910}, {128, 128, 2, 0.60, 1000}, {256, 256, 1, 1.17, 1210}};
+    {32, 128, 4, 0.375, 4.1, 530}, {32, 256, 2, 0.40, 5.9, 350}, {64, 128, 3, 0.45, 4.5, 560},
+    {64, 256, 2, 1.12, 6.2, 660}, {128, 128, 2, 0.385, 5.9, 940}, {256, 256, 1, 1.31, 14.9, 1460}};
 constexpr int kLinearTileCount = sizeof(kLinearTiles) / sizeof(kLinearTiles[0]);
 struct LinearPlan { int tile, splits; };        // tile -1: linear_rows_kernel
 
@@ -476,12 +479,12 @@ static LinearPlan plan_linear(int64_t m, int64_t n, int64_t k) {
             if (splits > 1 && (tiles * splits > 768 || blocks < 2 * splits)) break;
             const double groups = tiles * splits, per = std::ceil(blocks / splits);
             const double compute = std::ceil(groups / 256) * per * (2.0 * l.bm * l.bn * 64) / (l.tflops * 1e6 / 256);
-            const double wait = std::ceil(groups / (256.0 * l.resident)) * per * l.block_us;
-            // a stream of weights is fastest from one or two workgroups per compute unit; what all tiles load comes through the L2s
-            const double memory = 2.0 * ((double)n * k + (double)m * k) / 5.0e6 * (groups > 512 ? 1.1 : groups < 256 ? 1.5 - groups / 512 : 1.0) +
-                                  2.0 * tiles * (l.bm + l.bn) * k / 4.0e7;
-            const double join = splits > 1 ? 3.0 + (double)splits * m * n * 8 / 4.0e6 : 0.0;
-            const double us = std::max(std::max(compute, wait), memory) + join;
+            const double rounds = groups / (256.0 * l.resident), wait = std::ceil(rounds) * per * l.block_us;
+            // weights, x and the result from and to memory, slower from few workgroups; what all tiles load, through the L2s
+            const double spread = groups < 384 ? 1.0 + (384 - groups) / 1385 : 1.0;
+            const double memory = (2.0 * ((double)n * k + (double)m * k) * spread + 3.4 * (double)m * n) / 8.1e6 + 2.0 * tiles * (l.bm + l.bn) * k / 3.8e7;
+            const double join = splits > 1 ? 2.65 + (double)splits * m * n * 8 / 5.3e6 : 0.0;
+            const double us = std::max(std::max(compute, wait), memory) + std::max(rounds, 1.0) * l.tile_us + join;
             if (us < least) { least = us; best = {t, splits}; }
         }
     }
@@ -490,9 +493,8 @@ static LinearPlan plan_linear(int64_t m, int64_t n, int64_t k) {
 static int64_t part_stride_of(int64_t n) { return (n + 3) & ~3ll; }
 
 template <class T>
-static int launch_linear(LinearParams &p, void *workspace, void *stream) {
+static int launch_linear(LinearParams &p, LinearPlan plan, void *workspace, void *stream) {
     const char *what = "bpe_linear launch";
-    LinearPlan plan = plan_linear(p.m, p.n, p.k);
     p.splits = 1;
     const bool direct = p.x_stride % 8 == 0 && p.w_stride % 8 == 0 && !(((uintptr_t)p.x | (uintptr_t)p.w) & 15);
     // (rows at odd addresses cost linear_rows_kernel more than they cost a tile: 1 x 50256 x 1023 48 us and in tiles 34)
@@ -540,10 +542,11 @@ static int linear_sizes_ok(int64_t m, int64_t n, int64_t k) {
     return 1;
 }
 
+static int64_t linear_need(const LinearPlan &plan, int64_t m, int64_t n) { return plan.splits > 1 ? 4 * (int64_t)plan.splits * m * part_stride_of(n) : 0; }
+
 extern "C" int64_t bpe_linear_workspace_bytes(int64_t m, int64_t n, int64_t k) {
     if (!linear_sizes_ok(m, n, k)) return BPE_ERR_SIZE;
-    const LinearPlan plan = plan_linear(m, n, k);
-    return plan.splits > 1 ? 4 * (int64_t)plan.splits * m * part_stride_of(n) : 0;
+    return linear_need(plan_linear(m, n, k), m, n);
 }
 
 extern "C" int bpe_linear(const void *x, int64_t x_stride, const void *weight, int64_t weight_stride, int dtype, int64_t m, int64_t n,
@@ -560,7 +563,8 @@ extern "C" int bpe_linear(const void *x, int64_t x_stride, const void *weight, i
         set_error("bpe_linear: a stride is shorter than a row");
         return BPE_ERR_SIZE;
     }
-    const int64_t need = bpe_linear_workspace_bytes(m, n, k);
+    const LinearPlan plan = plan_linear(m, n, k);
+    const int64_t need = linear_need(plan, m, n);
     if (need > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) {
         set_error("workspace must be 256-byte aligned and hold %lld bytes (got %lld)", (long long)need, (long long)workspace_bytes);
         return BPE_ERR_WORKSPACE;
@@ -578,5 +582,5 @@ extern "C" int bpe_linear(const void *x, int64_t x_stride, const void *weight, i
     p.bias = bias; p.bias_dtype = bias_dtype; p.activation = activation;
     p.residual = residual; p.residual_stride = residual_stride;
     p.out = out; p.out_stride = out_stride; p.out_dtype = out_dtype;
-    return dtype == BPE_BF16 ? launch_linear<Bf16>(p, workspace, stream) : launch_linear<F16>(p, workspace, stream);
+    return dtype == BPE_BF16 ? launch_linear<Bf16>(p, plan, workspace, stream) : launch_linear<F16>(p, plan, workspace, stream);
 }

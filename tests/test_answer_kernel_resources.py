@@ -37,7 +37,7 @@ def test_no_kernel_needs_scratch_memory(usage):
 
 def test_tiles_fit_as_often_as_the_estimate_says(usage):
     text = open(os.path.join(CSRC, "bpe_linear.hip")).read()
-    tiles = re.findall(r"\{(\d+), (\d+), (\d+), [\d.]+, \d+\}", text)
+    tiles = re.findall(r"\{(\d+), (\d+), (\d+), [\d.]+, [\d.]+, \d+\}", text)
     assert len(tiles) == 6
     for bm, bn, resident in tiles:
         kernels = [u for k, u in usage.items() if f"linear_block_kernel" in k and f"Li{bm}ELi{bn}E" in k and "Lb1E" in k]
