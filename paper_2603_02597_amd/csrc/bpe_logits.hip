@@ -252,8 +252,8 @@ __device__ __forceinline__ uint64_t bound_of_best(TopShared &sh, int count, int 
                     if (!found) before += in[q];
                 }
                 sh.low = low + ((uint64_t)bin << shift);
-                const uint64_t end = sh.low + (((uint64_t)1 << shift) - 1);
-                sh.high = end < high ? end : high;
+                const uint64_t width = ((uint64_t)1 << shift) - 1;                // (low + width may pass 64 bits)
+                sh.high = high - sh.low < width ? high : sh.low + width;
                 sh.above = (int)before;
                 sh.n_few = (int)(before + there);
             }

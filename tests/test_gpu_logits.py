@@ -356,3 +356,14 @@ def test_no_rows(B):
     B.bpe_adjust_logits(empty, torch.empty(0, 50, device="cuda"))
     B.bpe_top_tokens(empty, torch.empty(0, 3, dtype=torch.int32, device="cuda"), torch.empty(0, 3, device="cuda"),
                      torch.empty(B.bpe_top_tokens_workspace_bytes(0, 50, 3), dtype=torch.uint8, device="cuda"))
+
+
+def test_nan_in_many_places(B):
+    """Rows of mostly NaN: the lowest indexes of NaN come first, and everything is NaN."""
+    import torch
+    x = torch.randn(3, 30000, device="cuda", generator=torch.Generator(device="cuda").manual_seed(4))
+    x[0] = float("nan")
+    x[1, 7::2] = float("nan")
+    ids, lp, lse = (t.cpu().numpy() for t in _top(B, torch, x, 40))
+    assert np.array_equal(ids[0], np.arange(40)) and np.array_equal(ids[1], 7 + 2 * np.arange(40))
+    assert np.isnan(lp[:2]).all() and np.isnan(lse[:2]).all() and np.isfinite(lp[2]).all()
