@@ -505,7 +505,7 @@ static int launch_linear(LinearParams &p, LinearPlan plan, void *workspace, void
     const int64_t bm = far ? 64 : kLinearTiles[plan.tile].bm, bn = far ? 64 : kLinearTiles[plan.tile].bn;
     p.splits = far ? 1 : plan.splits;
     const int64_t grid = tile_grid((p.m + bm - 1) / bm, (p.n + bn - 1) / bn, p.splits);
-    if (grid > 0x7FFFFFFF) { set_error("bpe_linear: m %d and n %d are too large together", p.m, p.n); return BPE_ERR_SIZE; }
+    if (grid >= kMaxThreads / kGroupThreads) { set_error("bpe_linear: m %d and n %d are too large together", p.m, p.n); return BPE_ERR_SIZE; }
     if (far) return launch(linear_tile_kernel<T>, dim3((unsigned)grid), kGroupThreads, p, stream, what);
     p.part = (float *)workspace;
     p.part_stride = (int32_t)part_stride_of(p.n);
@@ -577,7 +577,7 @@ extern "C" int bpe_linear(const void *x, int64_t x_stride, const void *weight, i
     }
     LinearParams p = {};
     p.x = (const uint16_t *)x; p.w = (const uint16_t *)weight;
-    p.x_stride = x_stride; p.w_stride = weight_stride;
+    p.x_stride = m > 1 ? x_stride : 0; p.w_stride = n > 1 ? weight_stride : 0;        // (of one row the stride says nothing)
     p.m = (int32_t)m; p.n = (int32_t)n; p.k = (int32_t)k;
     p.bias = bias; p.bias_dtype = bias_dtype; p.activation = activation;
     p.residual = residual; p.residual_stride = residual_stride;

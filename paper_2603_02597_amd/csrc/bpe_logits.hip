@@ -10,7 +10,7 @@ struct AdjustParams {
     const void *logits;
     void *out;
     int64_t logits_stride, out_stride;
-    int32_t rows, n_vocab;
+    int32_t row0, n_vocab;             // the launch's first row
     int32_t slice, slices;             // tokens of a row per workgroup, a multiple of 32
     bpe_logit_rules rules;
 };
@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(kAdjustThreads) adjust_kernel(AdjustParams p) 
     typedef uint32_t Counts __attribute__((ext_vector_type(kPer)));
     __shared__ __attribute__((aligned(32))) uint32_t count[LISTS ? kAdjustSlice : 1];
     const bpe_logit_rules &r = p.rules;
-    const int row = blockIdx.x / p.slices, first = blockIdx.x % p.slices * p.slice, last = min(first + p.slice, p.n_vocab), tid = threadIdx.x;
+    const int row = p.row0 + blockIdx.x / p.slices, first = blockIdx.x % p.slices * p.slice, last = min(first + p.slice, p.n_vocab), tid = threadIdx.x;
     const typename IN::raw *in = (const typename IN::raw *)p.logits + row * p.logits_stride;
     typename OUT::raw *out = (typename OUT::raw *)p.out + row * p.out_stride;
     int bias_begin = 0, bias_end = 0;
@@ -184,7 +184,7 @@ struct TopPart { float largest, sum, bound; int32_t words; };
 struct TopParams {
     const void *logits;
     int64_t logits_stride;
-    int32_t rows, n_vocab, k;
+    int32_t row0, n_vocab, k;                // the launch's first row
     int32_t parts, part_len, part_keep;      // a row is cut into so many parts of part_len logits, each leaves up to part_keep words
     int32_t *ids;
     float *logprobs, *lse;
@@ -393,7 +393,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) top_part_kernel(TopParams p) {
     typedef typename IN::raw Vec __attribute__((ext_vector_type(kPer), aligned(sizeof(typename IN::raw))));
     __shared__ __attribute__((aligned(16))) TopShared sh;
     const int tid = threadIdx.x, lane = tid & 63;
-    const int row = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
+    const int row = p.row0 + blockIdx.x / p.parts, part = blockIdx.x % p.parts;
     const int first = part * p.part_len, last = min(first + p.part_len, p.n_vocab);
     const typename IN::raw *in = (const typename IN::raw *)p.logits + row * p.logits_stride;
     if (tid == 0) sh.n = 0;
@@ -519,7 +519,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) top_part_kernel(TopParams p) {
 // The best of the parts' best: none is below the highest of the parts' bounds.
 __global__ void __launch_bounds__(kTopThreads) top_join_kernel(TopParams p) {
     __shared__ __attribute__((aligned(16))) TopShared sh;
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, row = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, row = p.row0 + blockIdx.x;
     const TopPart *left = p.left + (int64_t)row * p.parts;
     float bound = kLowest, largest = -__builtin_inff(), sum = 0.0f;
     for (int i = tid; i < p.parts; i += kTopThreads) {
@@ -605,7 +605,6 @@ extern "C" int bpe_adjust_logits(const void *logits, int64_t logits_stride, int 
     p.out = out;
     p.logits_stride = logits_stride;
     p.out_stride = out_stride;
-    p.rows = (int32_t)rows;
     p.n_vocab = (int32_t)n_vocab;
     const bool lists = p.rules.n_history > 0 || p.rules.n_bias > 0;
     // As many workgroups as are on the chip at once, if the slices can be as long: 64 rows of 100256 with lists 12.6 us, in twice as
@@ -613,7 +612,6 @@ extern "C" int bpe_adjust_logits(const void *logits, int64_t logits_stride, int 
     const int64_t per_row = std::max<int64_t>(512 / rows, (n_vocab + kAdjustSlice - 1) / kAdjustSlice);
     p.slice = (int32_t)std::max<int64_t>(((n_vocab + per_row - 1) / per_row + 31) & ~31ll, 2048);
     p.slices = (int32_t)((n_vocab + p.slice - 1) / p.slice);
-    if (rows * p.slices > 0x7FFFFFFF) { set_error("bpe_adjust_logits: rows %lld and n_vocab %lld are too large together", (long long)rows, (long long)n_vocab); return BPE_ERR_SIZE; }
     void (*kernel)(AdjustParams) = nullptr;
 #define ADJUST(IN, OUT) kernel = lists ? adjust_kernel<IN, OUT, true> : adjust_kernel<IN, OUT, false>
     if (dtype == BPE_F32) ADJUST(F32, F32);
@@ -622,7 +620,13 @@ extern "C" int bpe_adjust_logits(const void *logits, int64_t logits_stride, int 
     else if (out_dtype == BPE_F32) ADJUST(F16, F32);
     else ADJUST(F16, F16);
 #undef ADJUST
-    return launch(kernel, dim3((unsigned)(rows * p.slices)), kAdjustThreads, p, stream, "bpe_adjust_logits launch");
+    const int64_t at_once = (kMaxThreads - 1) / kAdjustThreads / p.slices;         // (2^30 tokens are 65,536 slices)
+    for (int64_t row = 0; row < rows; row += at_once) {
+        p.row0 = (int32_t)row;
+        const int rc_launch = launch(kernel, dim3((unsigned)(std::min(at_once, rows - row) * p.slices)), kAdjustThreads, p, stream, "bpe_adjust_logits launch");
+        if (rc_launch != BPE_OK) return rc_launch;
+    }
+    return BPE_OK;
 }
 
 static int check_top(int64_t rows, int64_t n_vocab, int64_t k) {
@@ -666,21 +670,25 @@ extern "C" int bpe_top_tokens(const void *logits, int64_t logits_stride, int dty
     TopParams p = {};
     p.logits = logits;
     p.logits_stride = logits_stride;
-    p.rows = (int32_t)rows;
     p.n_vocab = (int32_t)n_vocab;
     p.k = (int32_t)k;
     p.ids = ids;
     p.logprobs = logprobs;
     p.lse = lse;
     const int64_t parts = top_parts(rows, n_vocab, k);
-    if (rows * parts > 0x7FFFFFFF) { set_error("bpe_top_tokens: rows out of range (%lld)", (long long)rows); return BPE_ERR_SIZE; }
     p.parts = (int32_t)parts;
     p.part_len = (int32_t)(((n_vocab + parts - 1) / parts + 7) & ~7ll);
     p.kept = (uint64_t *)workspace;
     p.part_keep = (int32_t)part_keep(parts, k);
     p.left = (TopPart *)((char *)workspace + align256l(8 * rows * parts * p.part_keep));
-    const int rc = launch(dtype == BPE_F32 ? top_part_kernel<F32> : dtype == BPE_BF16 ? top_part_kernel<Bf16> : top_part_kernel<F16>,
-                          dim3((unsigned)(rows * parts)), kTopThreads, p, stream, "bpe_top_tokens launch");
-    if (rc != BPE_OK || parts == 1) return rc;
-    return launch(top_join_kernel, dim3((unsigned)rows), kTopThreads, p, stream, "bpe_top_tokens launch");
+    const int64_t at_once = (kMaxThreads - 1) / kTopThreads / parts;
+    for (int64_t row = 0; row < rows; row += at_once) {
+        const int64_t n = std::min(at_once, rows - row);
+        p.row0 = (int32_t)row;
+        int rc = launch(dtype == BPE_F32 ? top_part_kernel<F32> : dtype == BPE_BF16 ? top_part_kernel<Bf16> : top_part_kernel<F16>,
+                        dim3((unsigned)(n * parts)), kTopThreads, p, stream, "bpe_top_tokens launch");
+        if (rc == BPE_OK && parts > 1) rc = launch(top_join_kernel, dim3((unsigned)n), kTopThreads, p, stream, "bpe_top_tokens launch");
+        if (rc != BPE_OK) return rc;
+    }
+    return BPE_OK;
 }

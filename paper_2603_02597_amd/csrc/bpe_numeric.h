@@ -35,6 +35,8 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_wave_barrier();
 }
 
+constexpr int64_t kMaxThreads = 1ll << 32;      // of a launch: fewer
+
 // One launch of a kernel whose only argument is its parameter block.
 template <class P>
 inline int launch(void (*kernel)(P), dim3 grid, int block, P &p, void *stream, const char *what) {

@@ -358,6 +358,51 @@ def test_no_rows(B):
                      torch.empty(B.bpe_top_tokens_workspace_bytes(0, 50, 3), dtype=torch.uint8, device="cuda"))
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_many_biases_of_few_tokens(B, dtype):
+    """Lists of up to 5,000 entries for 300 tokens: the last entry of a token counts, in place too, with penalties and masks."""
+    import torch
+    rng = np.random.default_rng(21)
+    rows, vocab = 4, 20000
+    lengths = [5000, 0, 1025, 1024]
+    off = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32)
+    ids = (rng.integers(0, 300, off[-1]) * 61).astype(np.int32)
+    ids[::97] = -4
+    bias = (ids, rng.standard_normal(ids.size).astype(np.float32), off)
+    history = _lists(rng, rows, [4000, 10, 0, 600], vocab)
+    masks = rng.integers(-2**31, 2**31, (rows, (vocab + 31) // 32)).astype(np.int32)
+    logits = torch.from_numpy(rng.standard_normal((rows, vocab)).astype(np.float32)).cuda().to(getattr(torch, dtype))
+    rep, pres = np.full(rows, 1.3, dtype=np.float32), np.full(rows, 0.7, dtype=np.float32)
+    want = _reference(logits.float().cpu().numpy(), vocab, history, bias, masks, None, rep, None, pres)
+    got = _adjust(B, torch, logits, dtype, vocab, history, bias, masks, None, rep, None, pres)
+    _check_adjusted(got, logits, want, dtype)
+    again = _adjust(B, torch, logits, dtype, vocab, history, bias, masks, None, rep, None, pres, out=logits)
+    assert torch.equal(again, got)
+
+
+def test_more_rows_than_a_launch_holds(B):
+    """A launch has fewer than 2^32 threads: the rows behind that many go into another one."""
+    import torch
+    rows, vocab = 4200000, 8
+    g = torch.Generator(device="cuda").manual_seed(1)
+    logits = torch.randn(rows, vocab, generator=g, device="cuda").bfloat16()
+    masks = torch.tensor([[0x5A]], dtype=torch.int32, device="cuda")
+    out = torch.empty_like(logits)
+    B.bpe_adjust_logits(logits, out, masks=masks, mask_index=torch.zeros(rows, dtype=torch.int32, device="cuda"))
+    keep = torch.tensor([0x5A >> v & 1 for v in range(vocab)], dtype=torch.bool, device="cuda")
+    assert torch.equal(out, torch.where(keep, logits, torch.full_like(logits, float("-inf"))))
+    rows = 16800000
+    logits = torch.randint(0, 100, (rows, 4), generator=g, device="cuda").bfloat16()
+    ids = torch.empty(rows, 1, dtype=torch.int32, device="cuda")
+    lp = torch.empty(rows, 1, device="cuda")
+    B.bpe_top_tokens(logits, ids, lp, torch.empty(B.bpe_top_tokens_workspace_bytes(rows, 4, 1), dtype=torch.uint8, device="cuda"))
+    best = logits.max(1, keepdim=True)
+    first = (logits == best.values).int().argmax(1, keepdim=True)
+    assert torch.equal(ids.long(), first)
+    want = logits.float().log_softmax(1).gather(1, first)
+    assert float((lp - want).abs().max()) <= 600 * U + 4 * U * 110
+
+
 def test_nan_in_many_places(B):
     """Rows of mostly NaN: the lowest indexes of NaN come first, and everything is NaN."""
     import torch
