@@ -122,6 +122,16 @@ __device__ __forceinline__ void put4(const LinearParams &p, int i, int j, F4 v) 
 typedef uint32_t U4Any __attribute__((ext_vector_type(4), aligned(2)));
 __device__ __forceinline__ U4 load16(const uint16_t *at) { return *(const U4Any *)at; }
 
+// Eight elements without the first `over`, zeros in their place at the end.
+__device__ __forceinline__ U4 shift_out(U4 eight, int over) {
+    typedef uint64_t Two __attribute__((ext_vector_type(2)));
+    const Two v = __builtin_bit_cast(Two, eight);
+    const uint32_t shift = 16u * (uint32_t)(over & 3);
+    const uint64_t low = over < 4 ? v[0] : v[1], high = over < 4 ? v[1] : 0;
+    Two o = {low >> shift | (shift ? high << (64 - shift) : 0), high >> shift};
+    if (over >= 8) o = Two{0, 0};
+    return __builtin_bit_cast(U4, o);
+}
 // Eight elements of a row from column t on, zeros behind the row's end: the row's last eight at most, shifted.  No branch for k >= 8.
 __device__ __forceinline__ U4 load_tail(const uint16_t *row, int t, int k) {
     if (k < 8) {
@@ -132,13 +142,7 @@ __device__ __forceinline__ U4 load_tail(const uint16_t *row, int t, int k) {
         return __builtin_bit_cast(U4, v);
     }
     const int over = max(t - (k - 8), 0);                 // elements of the eight that lie behind the end
-    typedef uint64_t Two __attribute__((ext_vector_type(2)));
-    const Two v = __builtin_bit_cast(Two, load16(row + (t - over)));
-    const uint32_t shift = 16u * (uint32_t)(over & 3);
-    const uint64_t low = over < 4 ? v[0] : v[1], high = over < 4 ? v[1] : 0;
-    Two o = {low >> shift | (shift ? high << (64 - shift) : 0), high >> shift};
-    if (over >= 8) o = Two{0, 0};
-    return __builtin_bit_cast(U4, o);
+    return shift_out(load16(row + (t - over)), over);
 }
 
 // A few rows of x: the call is as long as reading weight takes, so weight goes from memory straight into the matrix cores'
@@ -166,6 +170,16 @@ __global__ void __launch_bounds__(kGroupThreads) linear_rows_kernel(LinearParams
 #pragma unroll
         for (int h = 0; h < 2; ++h) acc = mma16<T>(wf[u][h], xf[u][h], acc);
     };
+    // the columns behind the last whole step
+    const bool tail = wv == kWavesPerGroup - 1 && (p.k & 63);
+    U4 w_tail[2], x_tail[2];
+    if (tail) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            w_tail[h] = load_tail(w, (p.k & ~63) + 32 * h + group, p.k);
+            x_tail[h] = load_tail(x, (p.k & ~63) + 32 * h + group, p.k);
+        }
+    }
 #pragma unroll
     for (int u = 0; u < kRowsAhead; ++u)
         if (from + u < to) load(u, from + u);
@@ -183,13 +197,9 @@ __global__ void __launch_bounds__(kGroupThreads) linear_rows_kernel(LinearParams
                 multiply(u);
                 if (step + kRowsAhead + u < to) load(u, step + kRowsAhead + u);
             }
-    if (wv == kWavesPerGroup - 1 && (p.k & 63)) {
+    if (tail) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            wf[0][h] = load_tail(w, (p.k & ~63) + 32 * h + group, p.k);
-            xf[0][h] = load_tail(x, (p.k & ~63) + 32 * h + group, p.k);
-        }
-        multiply(0);
+        for (int h = 0; h < 2; ++h) acc = mma16<T>(w_tail[h], x_tail[h], acc);
     }
     part[wv][lane] = acc;
     __syncthreads();
@@ -253,14 +263,18 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
     // Sixteen-byte groups of a row lie in LDS at their index XOR the row's last three bits, so that eight neighbouring rows
     // read at one index meet eight different groups of banks.
     const int row8 = lane >> 3, group = (lane & 7) ^ row8;
-    // this part's blocks of 64 columns; the last part also has what is left behind the last whole block
-    const int all_blocks = p.k >> 6, block0 = (int)((int64_t)all_blocks * split / p.splits), blocks = (int)((int64_t)all_blocks * (split + 1) / p.splits) - block0;
-    const char *xb = (const char *)(p.x + i0 * p.x_stride + 64 * (int64_t)block0), *wb = (const char *)(p.w + j0 * p.w_stride + 64 * (int64_t)block0);
-    uint32_t at[kLoads];
+    // this part's blocks of 64 columns; the last one of all may be cut off
+    const int all_blocks = (p.k + 63) >> 6, block0 = (int)((int64_t)all_blocks * split / p.splits), blocks = (int)((int64_t)all_blocks * (split + 1) / p.splits) - block0;
+    const int cut = split == p.splits - 1 ? p.k & 63 : 0;             // the columns of a last block that is cut off, or 0
+    // Columns of this lane's group of a cut block that lie behind the row's end, or behind its last whole group where rows are aligned:
+    // the group is loaded from so much further in front (eight columns in front of the block at most, and k >= 8) and mended in LDS.
+    const int over = max(8 * group + 8 - (DIRECT ? cut & ~7 : cut), 0);
+    const char *xb = (const char *)(p.x + i0 * p.x_stride + 64 * (int64_t)block0 - 8), *wb = (const char *)(p.w + j0 * p.w_stride + 64 * (int64_t)block0 - 8);
+    uint32_t at[kLoads];               // (from eight columns in front of the block on)
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
         const int row = ((q < kLoadsX ? q : q - kLoadsX) * NW + wv) * 8 + row8;
-        at[q] = 2u * (uint32_t)((q < kLoadsX ? min(row, p.m - 1 - i0) * (int)p.x_stride : min(row, p.n - 1 - j0) * (int)p.w_stride) + 8 * group);
+        at[q] = 2u * (uint32_t)((q < kLoadsX ? min(row, p.m - 1 - i0) * (int)p.x_stride : min(row, p.n - 1 - j0) * (int)p.w_stride) + 8 * group + 8);
     }
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wv * 1024;
     U4 held[DIRECT ? 1 : kLoads];      // rows at any alignment pass through registers
@@ -301,6 +315,30 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    auto step_back = [&]() {
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q) at[q] -= 2u * (uint32_t)over;
+    };
+    // Zeros behind the row's end in a cut block that has arrived.
+    auto mend = [&](int x_slot, int w_slot) {
+        if (over) {
+#pragma unroll
+            for (int q = 0; q < kLoads; ++q) {
+                U4 *mine = (U4 *)(lds + (q < kLoadsX ? x_slot + q * (NW * 1024) : w_slot + (q - kLoadsX) * (NW * 1024)) + wv * 1024 + 16 * lane);
+                if constexpr (DIRECT) {
+                    U4 v = {0, 0, 0, 0};
+                    if (8 * group < cut) {
+                        const int row = ((q < kLoadsX ? q : q - kLoadsX) * NW + wv) * 8 + row8;
+                        v = load_tail(q < kLoadsX ? p.x + min(i0 + row, p.m - 1) * p.x_stride : p.w + min(j0 + row, p.n - 1) * p.w_stride, p.k - cut + 8 * group, p.k);
+                    }
+                    *mine = v;
+                } else {
+                    *mine = shift_out(*mine, over);
+                }
+            }
+        }
+        __syncthreads();
+    };
     constexpr std::integral_constant<int, 0> none;
     constexpr std::integral_constant<int, 1> second;
     constexpr std::integral_constant<int, kLoadsX> x_end;
@@ -311,13 +349,16 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
         // in the first half of block t already: loads then come evenly, and may take longer.
         constexpr bool kThird = XS == 3;
         int x0 = 0, x1 = kX, x2 = XS == 3 ? 2 * kX : 0, w0 = XS * kX, w1 = w0 + kW;       // of blocks t, t + 1, t + 2
+        if (cut && blocks == 1) step_back();
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) load_part(x0, w0, 0, q);
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) store_part(x0, w0, q);
         wait_and_meet<0>();
+        if (cut && blocks == 1) mend(x0, w0);
 #pragma unroll
         for (int q = 0; q < kReads; ++q) read_part(x0, w0, 0, q);
+        if (cut && blocks == 2) step_back();
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) load_part(x1, w1, min(1, blocks - 1), q);
         if constexpr (kThird) {
@@ -327,9 +368,11 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
         for (int t = 0; t < blocks; ++t) {
             // (behind the last block: that block again, for nobody)
             const int t2 = min(t + 2, blocks - 1);
+            if (cut && t + 3 == blocks) step_back();
             if constexpr (kThird) phase(none, none, x_end, x_end, all, x0, w0, x2, 0, t2, 0, w1);
             else phase(none, none, none, none, all, x0, w0, 0, 0, 0, x1, w1);
             wait_and_meet<kThird && DIRECT ? kLoadsX : 0>();          // block t + 1 is there, and nobody reads block t any more
+            if (cut && t + 2 == blocks) mend(x1, w1);
             if constexpr (kThird) phase(second, x_end, all, none, x_end, x1, w1, 0, w0, t2, x2, 0);
             else phase(second, none, all, none, none, x1, w1, x0, w0, t2, 0, 0);
             const int x = x0, w = w0;
@@ -340,31 +383,6 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
             w1 = w;
         }
         wait_and_meet<0>();
-    }
-    // The columns behind the last whole block, filled up with zeros.
-    if (split == p.splits - 1 && (p.k & 63)) {
-        U4 last[kLoads];
-#pragma unroll
-        for (int q = 0; q < kLoads; ++q) {
-            const int row = ((q < kLoadsX ? q : q - kLoadsX) * NW + wv) * 8 + row8;
-            const uint16_t *from = q < kLoadsX ? p.x + min(i0 + row, p.m - 1) * p.x_stride : p.w + min(j0 + row, p.n - 1) * p.w_stride;
-            last[q] = load_tail(from, 64 * all_blocks + 8 * group, p.k);
-        }
-#pragma unroll
-        for (int q = 0; q < kLoads; ++q)
-            *(U4 *)(lds + (q < kLoadsX ? q * NW * 1024 : kX + (q - kLoadsX) * NW * 1024) + wv * 1024 + 16 * lane) = last[q];
-        __syncthreads();
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-#pragma unroll
-            for (int q = 0; q < kReads; ++q) read_part(0, kX, half, q);
-#pragma unroll
-            for (int q = 0; q < kProducts; ++q) {
-                const int s = q / (TM * TN), a = q / TN % TM, b = q % TN;
-                acc[a][b] = mma32<T>(frag[half][s][TM + b], frag[half][s][a], acc[a][b]);
-            }
-        }
-        __syncthreads();
     }
     // The result goes through LDS, 32 rows of a wavefront's part at a time, so that a row's columns leave next to each other:
     // the lanes hold one row each, four columns at a time.  (The padding of four columns spreads the rows over the banks.)
@@ -471,7 +489,7 @@ static LinearPlan plan_linear(int64_t m, int64_t n, int64_t k) {
     if (m <= 4 || (m <= 16 && n * k <= (1 << 24))) return {-1, 1};
     LinearPlan best = {0, 1};
     double least = 1e300;
-    const double blocks = (double)std::max<int64_t>(k >> 6, 1);
+    const double blocks = (double)std::max<int64_t>((k + 63) >> 6, 1);
     for (int t = 0; t < kLinearTileCount; ++t) {
         const LinearTile &l = kLinearTiles[t];
         const double tiles = (double)((m + l.bm - 1) / l.bm) * (double)((n + l.bn - 1) / l.bn);
@@ -500,8 +518,9 @@ static int launch_linear(LinearParams &p, LinearPlan plan, void *workspace, void
     // (rows at odd addresses cost linear_rows_kernel more than they cost a tile: 1 x 50256 x 1023 48 us and in tiles 34)
     if (plan.tile < 0 && !direct && (int64_t)p.n * p.k > (1 << 24)) plan = {0, 1};
     if (plan.tile < 0) return launch(linear_rows_kernel<T>, dim3((unsigned)(((int64_t)p.n + 15) / 16)), kGroupThreads, p, stream, what);
-    // A tile's rows are addressed by 32-bit offsets; rows that lie further apart take the simple kernel.
-    const bool far = p.x_stride >= (1 << 21) || p.w_stride >= (1 << 21);
+    // A tile's rows are addressed by 32-bit offsets, and every load is of eight columns: rows that lie further apart or are shorter
+    // take the simple kernel.
+    const bool far = p.x_stride >= (1 << 21) || p.w_stride >= (1 << 21) || p.k < 8;
     const int64_t bm = far ? 64 : kLinearTiles[plan.tile].bm, bn = far ? 64 : kLinearTiles[plan.tile].bn;
     p.splits = far ? 1 : plan.splits;
     const int64_t grid = tile_grid((p.m + bm - 1) / bm, (p.n + bn - 1) / bn, p.splits);

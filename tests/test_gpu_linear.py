@@ -212,3 +212,24 @@ def test_same_bits_again_on_another_stream_and_in_a_graph(B):
             torch.cuda.synchronize()
             assert torch.equal(outs[0], outs[2])
         assert torch.equal(outs[0], outs[1])
+
+
+@pytest.mark.parametrize("k", [1, 7, 8, 9, 15, 57, 63, 65, 71, 72, 100, 127, 129, 184, 197, 263, 321])
+@pytest.mark.parametrize("stride", ["rows of sixteen bytes", "rows next to each other"])
+def test_rows_that_end_inside_a_block(B, k, stride):
+    """Every way for k to end inside 64 columns, few blocks and many, NaN right behind a row, on tiles of every size."""
+    import torch
+    for m, n in ((3, 900), (30, 2000), (60, 5000), (130, 20000), (500, 700), (1100, 9000)):
+        print(f"[case] linear cut {m} {n} {k} {stride}", flush=True)
+        pad = -k % 8 if stride == "rows of sixteen bytes" else 0
+
+        def inside(seed, rows):
+            t = torch.full((rows * (k + pad) + 8,), float("nan"), dtype=torch.bfloat16, device="cuda")
+            view = t[:rows * (k + pad)].view(rows, k + pad)[:, :k]
+            view.copy_(_rand(torch, seed, rows, k, dtype=torch.bfloat16))
+            return view
+
+        x, w = inside(1, m), inside(2, n)
+        got = torch.full((m, n), float("nan"), device="cuda")
+        _call(B, torch, x, w, got)
+        _check(got, x, w, None, None, "none", "float32")
