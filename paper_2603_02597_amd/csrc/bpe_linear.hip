@@ -36,14 +36,37 @@ template <> __device__ __forceinline__ F4 mma16<F16>(U4 a, U4 b, F4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(F16x8, a), __builtin_bit_cast(F16x8, b), c, 0, 0, 0);
 }
 
-__device__ __forceinline__ float activate(float v, int activation) {
-    switch (activation) {
-        case BPE_ACT_RELU: return v > 0.0f ? v : (v != v ? v : 0.0f);
-        case BPE_ACT_GELU: return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
-        case BPE_ACT_GELU_TANH: return 0.5f * v * (1.0f + tanhf(0.79788456080286536f * (v + 0.044715f * v * v * v)));
-        case BPE_ACT_SILU: return v / (1.0f + expf(-v));
-        default: return v;
+// The activations without a branch, from the hardware's 2^x and reciprocal (a unit in the last place each); where the factor of v
+// is 0 they give their limit, 0, for -infinity too.
+__device__ __forceinline__ float scaled(float v, float factor) { return factor == 0.0f ? 0.0f : v * factor; }
+__device__ __forceinline__ float sigmoid_of(float minus_log2_odds) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(minus_log2_odds)); }
+__device__ __forceinline__ float relu(float v) { return v < 0.0f ? 0.0f : v; }
+// v (1 + erf(v / sqrt 2)) / 2 = max(v, 0) - |v| q with q = (1 - erf(|v| / sqrt 2)) / 2, by the approximation 7.1.26 of Abramowitz and
+// Stegun's handbook, which is good to 1.5e-7 of 1.
+__device__ __forceinline__ float gelu(float v) {
+    const float z = __builtin_fabsf(v) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * z);
+    const float series = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    return relu(v) - scaled(__builtin_fabsf(v), 0.5f * series * __builtin_amdgcn_exp2f(-1.44269504088896341f * z * z));
+}
+// v (1 + tanh u) / 2 = v / (1 + exp(-2 u))
+__device__ __forceinline__ float gelu_tanh(float v) {
+    return scaled(v, sigmoid_of(-2.0f * 1.44269504088896341f * 0.79788456080286536f * (v + 0.044715f * v * v * v)));
+}
+__device__ __forceinline__ float silu(float v) { return scaled(v, sigmoid_of(-1.44269504088896341f * v)); }
+
+template <int ROWS> __device__ __forceinline__ void activate(F4 (&v)[ROWS], int activation) {
+#define EACH(FUNCTION) \
+    _Pragma("unroll") for (int u = 0; u < ROWS; ++u) { \
+        _Pragma("unroll") for (int e = 0; e < 4; ++e) v[u][e] = FUNCTION(v[u][e]); \
+        __builtin_amdgcn_sched_barrier(0); /* (not all rows' intermediate values at once) */ \
     }
+    switch (activation) {
+        case BPE_ACT_RELU: EACH(relu); break;
+        case BPE_ACT_GELU: EACH(gelu); break;
+        case BPE_ACT_GELU_TANH: EACH(gelu_tanh); break;
+        case BPE_ACT_SILU: EACH(silu); break;
+    }
+#undef EACH
 }
 
 typedef float F4Any __attribute__((ext_vector_type(4), aligned(4)));
@@ -51,29 +74,55 @@ typedef uint16_t H4Any __attribute__((ext_vector_type(4), aligned(2)));
 
 __device__ __forceinline__ float out_to_float(const LinearParams &p, uint16_t v) { return p.out_dtype == BPE_BF16 ? to_float<Bf16>(v) : to_float<F16>(v); }
 __device__ __forceinline__ uint16_t out_from_float(const LinearParams &p, float v) { return p.out_dtype == BPE_BF16 ? from_float<Bf16>(v) : from_float<F16>(v); }
-__device__ __forceinline__ F4 bias_of(const LinearParams &p, int j) {          // of columns j .. j + 3, which exist
-    if (!p.bias) return F4{0, 0, 0, 0};
-    if (p.bias_dtype == BPE_F32) return *(const F4Any *)((const float *)p.bias + j);
-    const H4Any b = *(const H4Any *)((const uint16_t *)p.bias + j);
-    F4 v;
+__device__ __forceinline__ F4 bias_of(const LinearParams &p, int j) {          // of columns j .. j + 3, as far as they exist
+    F4 v = {0, 0, 0, 0};
+    if (!p.bias) return v;
+    if (j + 3 >= p.n) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = p.bias_dtype == BPE_BF16 ? to_float<Bf16>(b[e]) : to_float<F16>(b[e]);
+        for (int e = 0; e < 4; ++e)
+            if (j + e < p.n) v[e] = load_as_float(p.bias, j + e, p.bias_dtype);
+    } else if (p.bias_dtype == BPE_F32) {
+        v = *(const F4Any *)((const float *)p.bias + j);
+    } else {
+        const H4Any b = *(const H4Any *)((const uint16_t *)p.bias + j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = p.bias_dtype == BPE_BF16 ? to_float<Bf16>(b[e]) : to_float<F16>(b[e]);
+    }
     return v;
 }
-// The epilogue of columns j .. j + 3, as far as they exist, of ROWS rows that are `step` apart, as far as they do.  ACTIVATED: with any
-// activation; else without one.  (Every lane of a call takes the same branches but those at the edges.)
-template <int ROWS, bool ACTIVATED>
-__device__ __forceinline__ void put(const LinearParams &p, int i, int step, int j, F4 (&v)[ROWS]) {
+// What the residual holds for columns j .. j + 3, if all exist, of ROWS rows that are `step` apart: bytes as they are (16-bit ones in
+// the first half).  Rows behind the last repeat it.
+template <int ROWS> __device__ __forceinline__ void fetch(const LinearParams &p, int i, int step, int j, U4 (&res)[ROWS]) {
+    if (!p.residual || j + 3 >= p.n) return;
+    typedef uint32_t U2Any __attribute__((ext_vector_type(2), aligned(2)));
+    if (p.out_dtype == BPE_F32) {
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) res[u] = __builtin_bit_cast(U4, *(const F4Any *)((const float *)p.residual + min(i + u * step, p.m - 1) * p.residual_stride + j));
+    } else {
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) {
+            const U2Any r = *(const U2Any *)((const uint16_t *)p.residual + min(i + u * step, p.m - 1) * p.residual_stride + j);
+            res[u] = U4{r[0], r[1], 0, 0};
+        }
+    }
+}
+// The epilogue of these columns, as far as they exist, of these rows, as far as they do; `bias`: of bias_of, `res`: of fetch.
+// (Every lane of a call takes the same branches but those at the edges.)
+template <int ROWS>
+__device__ __forceinline__ void put(const LinearParams &p, int i, int step, int j, F4 (&v)[ROWS], F4 bias, const U4 (&res)[ROWS]) {
+    if (p.bias) {
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) v[u] += bias;
+    }
+    activate(v, p.activation);
     if (j + 3 >= p.n) {
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) {
-#pragma unroll 1
+            const int64_t row = i + u * step;
+#pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if (i + u * step >= p.m || j + e >= p.n) break;
-                const int64_t row = i + u * step;
-                float x = e == 0 ? v[u][0] : e == 1 ? v[u][1] : e == 2 ? v[u][2] : v[u][3];
-                if (p.bias) x += load_as_float(p.bias, j + e, p.bias_dtype);
-                if (ACTIVATED) x = activate(x, p.activation);
+                if (row >= p.m || j + e >= p.n) break;
+                float x = v[u][e];
                 if (p.residual) x += load_as_float(p.residual, row * p.residual_stride + j + e, p.out_dtype);
                 const int64_t at = row * p.out_stride + j + e;
                 if (p.out_dtype == BPE_F32) ((float *)p.out)[at] = x;
@@ -82,31 +131,25 @@ __device__ __forceinline__ void put(const LinearParams &p, int i, int step, int 
         }
         return;
     }
-    if (p.bias) {
-        const F4 b = bias_of(p, j);
+    if (p.residual) {
 #pragma unroll
-        for (int u = 0; u < ROWS; ++u) v[u] += b;
-    }
-    if (ACTIVATED && p.activation != BPE_ACT_NONE) {
+        for (int u = 0; u < ROWS; ++u) {
+            if (p.out_dtype == BPE_F32) {
+                v[u] += __builtin_bit_cast(F4, res[u]);
+            } else {
 #pragma unroll
-        for (int u = 0; u < ROWS; ++u)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[u][e] = activate(v[u][e], p.activation);
+                for (int e = 0; e < 4; ++e) v[u][e] += out_to_float(p, (uint16_t)(res[u][e / 2] >> 16 * (e % 2)));
+            }
+        }
     }
 #pragma unroll
     for (int u = 0; u < ROWS; ++u) {
-        const int64_t row = i + u * step, at = row * p.out_stride + j, from = row * p.residual_stride + j;
+        const int64_t row = i + u * step, at = row * p.out_stride + j;
         if (row >= p.m) break;
         if (p.out_dtype == BPE_F32) {
-            if (p.residual) v[u] += *(const F4Any *)((const float *)p.residual + from);
             *(F4Any *)((float *)p.out + at) = v[u];
         } else {
             H4Any o;
-            if (p.residual) {
-                o = *(const H4Any *)((const uint16_t *)p.residual + from);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[u][e] += out_to_float(p, o[e]);
-            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = out_from_float(p, v[u][e]);
             *(H4Any *)((uint16_t *)p.out + at) = o;
@@ -115,7 +158,9 @@ __device__ __forceinline__ void put(const LinearParams &p, int i, int step, int 
 }
 __device__ __forceinline__ void put4(const LinearParams &p, int i, int j, F4 v) {
     F4 one[1] = {v};
-    put<1, true>(p, i, 1, j, one);
+    U4 res[1];
+    fetch(p, i, 1, j, res);
+    put(p, i, 1, j, one, bias_of(p, j), res);
 }
 
 // Sixteen bytes at any even address: the hardware asks for no more.
@@ -248,13 +293,15 @@ __device__ __forceinline__ bool tile_of(int64_t tiles_m, int64_t tiles_n, int sp
 }
 static int64_t tile_grid(int64_t tiles_m, int64_t tiles_n, int splits) { return (tiles_m * tiles_n * splits + 7) / 8 * 8; }
 
+constexpr int lds_of_tile(int bm, int bn, int x_slots) { return 128 * (x_slots * bm + 2 * bn); }
+// (as many wavefronts on a SIMD as there are workgroups of four whose LDS a compute unit holds)
 template <class T, int BM, int BN, int WM, int WN, int XS, bool DIRECT>
-__global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParams p) {
+__global__ void __launch_bounds__(WM *WN *kWave, 163840 / lds_of_tile(BM, BN, XS)) linear_block_kernel(LinearParams p) {
     constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
     constexpr int kLoadsX = BM / 8 / NW, kLoadsW = BN / 8 / NW, kLoads = kLoadsX + kLoadsW;      // of eight rows of 64 columns
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "");
     constexpr int kX = BM * 128, kW = BN * 128;                        // bytes of a block's rows of x and of weight: XS and two of them
-    __shared__ __attribute__((aligned(1024))) char lds[XS * kX + 2 * kW];
+    __shared__ __attribute__((aligned(1024))) char lds[lds_of_tile(BM, BN, XS)];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int64_t tile_m, tile_n;
     int split;
@@ -365,14 +412,15 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
 #pragma unroll
             for (int q = 0; q < kLoadsX; ++q) store_part(x1, w1, q);
         }
-        for (int t = 0; t < blocks; ++t) {
+        auto step = [&](int t, auto near_end) {
+            constexpr bool kNearEnd = decltype(near_end)::value;
             // (behind the last block: that block again, for nobody)
             const int t2 = min(t + 2, blocks - 1);
-            if (cut && t + 3 == blocks) step_back();
+            if (kNearEnd && t + 3 == blocks) step_back();
             if constexpr (kThird) phase(none, none, x_end, x_end, all, x0, w0, x2, 0, t2, 0, w1);
             else phase(none, none, none, none, all, x0, w0, 0, 0, 0, x1, w1);
             wait_and_meet<kThird && DIRECT ? kLoadsX : 0>();          // block t + 1 is there, and nobody reads block t any more
-            if (cut && t + 2 == blocks) mend(x1, w1);
+            if (kNearEnd && t + 2 == blocks) mend(x1, w1);
             if constexpr (kThird) phase(second, x_end, all, none, x_end, x1, w1, 0, w0, t2, x2, 0);
             else phase(second, none, all, none, none, x1, w1, x0, w0, t2, 0, 0);
             const int x = x0, w = w0;
@@ -381,7 +429,12 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
             x2 = x;
             w0 = w1;
             w1 = w;
-        }
+        };
+        // (the steps that a cut block asks more of have a loop of their own: 4001 x 50256 x 4096 1,377 us, in one loop 1,409)
+        const int calm = cut ? blocks - 3 : blocks;
+        int t = 0;
+        for (; t < calm; ++t) step(t, std::false_type());
+        for (; t < blocks; ++t) step(t, std::true_type());
         wait_and_meet<0>();
     }
     // The result goes through LDS, 32 rows of a wavefront's part at a time, so that a row's columns leave next to each other:
@@ -389,38 +442,46 @@ __global__ void __launch_bounds__(WM *WN *kWave) linear_block_kernel(LinearParam
     constexpr int kCols = 32 * TN, kPitch = kCols + 4, kLanesPerRow = kCols / 4;
     static_assert(NW * 32 * kPitch * 4 <= XS * kX + 2 * kW, "the rows of all wavefronts fit the buffers");
     float *stage = (float *)lds + wv * (32 * kPitch);
-#pragma unroll
+    // a batch of rows at a time: their reads and their stores are under way together, and so is the residual of the next batch
+    constexpr int kStep = 64 / kLanesPerRow, kBatch = kStep < 4 ? 8 : 4, kRows = kBatch * kStep;
+    const int j = j0 + wn * kCols + 4 * (lane % kLanesPerRow), i = i0 + wm * (BM / WM) + lane / kLanesPerRow;
+    const float *mine = stage + lane / kLanesPerRow * kPitch + 4 * (lane % kLanesPerRow);
+    U4 res[kBatch], next[kBatch];
+    F4 bias = {0, 0, 0, 0};
+    if (p.splits == 1) {
+        bias = bias_of(p, j);
+        fetch(p, i, kStep, j, next);
+    }
+#pragma unroll 1
     for (int a = 0; a < TM; ++a) {
 #pragma unroll
-        for (int b = 0; b < TN; ++b)
+        for (int a_is = 0; a_is < TM; ++a_is) {           // (the registers of acc have no index at run time)
+            if (a != a_is) continue;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                *(F4 *)(stage + (lane & 31) * kPitch + 32 * b + 8 * e + 4 * (lane >> 5)) =
-                    F4{acc[a][b][4 * e], acc[a][b][4 * e + 1], acc[a][b][4 * e + 2], acc[a][b][4 * e + 3]};
+            for (int b = 0; b < TN; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    *(F4 *)(stage + (lane & 31) * kPitch + 32 * b + 8 * e + 4 * (lane >> 5)) =
+                        F4{acc[a_is][b][4 * e], acc[a_is][b][4 * e + 1], acc[a_is][b][4 * e + 2], acc[a_is][b][4 * e + 3]};
+        }
         wave_sync();
-        // a batch of rows at a time: their reads and their stores are under way together
-        constexpr int kStep = 64 / kLanesPerRow, kBatch = 32 / kStep < 8 ? 32 / kStep : 8;
-        const int j = j0 + wn * kCols + 4 * (lane % kLanesPerRow), i = i0 + wm * (BM / WM) + 32 * a + lane / kLanesPerRow;
-        const float *mine = stage + lane / kLanesPerRow * kPitch + 4 * (lane % kLanesPerRow);
-        if (p.splits > 1 || p.activation == BPE_ACT_NONE) {
 #pragma unroll 1
-            for (int r = 0; r < 32; r += kBatch * kStep) {
-                F4 v[kBatch];
+        for (int r = 0; r < 32; r += kRows) {
+            F4 v[kBatch];
 #pragma unroll
-                for (int u = 0; u < kBatch; ++u) v[u] = *(const F4 *)(mine + (r + u * kStep) * kPitch);
-                if (j >= p.n) continue;
-                if (p.splits > 1) {
+            for (int u = 0; u < kBatch; ++u) v[u] = *(const F4 *)(mine + (r + u * kStep) * kPitch);
+            if (j >= p.n) continue;
+            const int row = i + 32 * a + r;
+            if (p.splits > 1) {
 #pragma unroll
-                    for (int u = 0; u < kBatch; ++u)
-                        if (i + r + u * kStep < p.m) *(F4 *)(p.part + ((int64_t)split * p.m + i + r + u * kStep) * p.part_stride + j) = v[u];
-                } else {
-                    put<kBatch, false>(p, i + r, kStep, j, v);
-                }
+                for (int u = 0; u < kBatch; ++u)
+                    if (row + u * kStep < p.m) *(F4 *)(p.part + ((int64_t)split * p.m + row + u * kStep) * p.part_stride + j) = v[u];
+            } else {
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) res[u] = next[u];
+                fetch(p, row + kRows, kStep, j, next);
+                put(p, row, kStep, j, v, bias, res);
             }
-        } else if (j < p.n) {
-#pragma unroll 1
-            for (int r = 0; r < 32; r += kStep)
-                if (i + r < p.m) put4(p, i + r, j, *(const F4 *)(mine + r * kPitch));
         }
         wave_sync();
     }

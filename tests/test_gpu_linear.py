@@ -233,3 +233,35 @@ def test_rows_that_end_inside_a_block(B, k, stride):
         got = torch.full((m, n), float("nan"), device="cuda")
         _call(B, torch, x, w, got)
         _check(got, x, w, None, None, "none", "float32")
+
+
+def test_activations_of_infinity_and_nan(B):
+    """Their limits at both ends, which all four have; NaN stays NaN."""
+    import torch
+    x, w = torch.zeros(40, 16, dtype=torch.float16, device="cuda"), torch.zeros(70, 16, dtype=torch.float16, device="cuda")
+    bias = torch.zeros(70, device="cuda")
+    bias[3], bias[4], bias[5] = float("inf"), float("-inf"), float("nan")
+    bias[69] = float("-inf")
+    for m in (1, 40):
+        for act in ("relu", "gelu", "gelu_tanh", "silu"):
+            out = torch.empty(m, 70, device="cuda")
+            _call(B, torch, x[:m], w, out, bias=bias, activation=act)
+            got = out.cpu().numpy()
+            assert np.isposinf(got[:, 3]).all() and (got[:, 4] == 0).all() and np.isnan(got[:, 5]).all(), act
+            assert (np.delete(got, [3, 5], axis=1) == 0).all(), act
+
+
+def test_activations_over_their_range(B):
+    """Of 40,000 values from -30 to 30: the sum is exact here, so the tolerance is the functions' and the rounding alone (the cut
+    series for gelu is good to 1.5e-7 / 2 of the argument)."""
+    import torch
+    n = 40000
+    x, w = torch.zeros(2, 8, dtype=torch.bfloat16, device="cuda"), torch.zeros(n, 8, dtype=torch.bfloat16, device="cuda")
+    bias = torch.linspace(-30, 30, n, device="cuda")
+    v = bias.double().cpu().numpy()
+    for act in ("relu", "gelu", "gelu_tanh", "silu"):
+        out = torch.empty(2, n, device="cuda")
+        _call(B, torch, x, w, out, bias=bias, activation=act)
+        want = _act(v, act)
+        tol = 4e-6 * np.abs(want) + 2.0 ** -24 * np.abs(want) + (0.75e-7 + 2 * 2.0 ** -24) * np.abs(v)
+        assert (np.abs(out.double().cpu().numpy() - want) <= tol).all(), act
