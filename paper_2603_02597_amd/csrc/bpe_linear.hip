@@ -536,11 +536,11 @@ __global__ void __launch_bounds__(kGroupThreads) linear_join_kernel(LinearParams
 // row: its sides, how many of its workgroups a compute unit holds, us for a block of 64 columns when a workgroup waits for
 // its loads alone, us for its first loads and its result, and the TFLOP/s of the whole chip when nothing else bounds it.  The
 // numbers are fitted to the times of all tiles and parts on 93 sizes (m 5 to 8192, n 256 to 128000, k 64 to 4096); there the choice takes
-// 1.7 % longer than the best one on average, 23 % at worst.
+// 1.6 % longer than the best one on average, 19 % at worst.
 struct LinearTile { int bm, bn, resident; double block_us, tile_us, tflops; };
 constexpr LinearTile kLinearTiles[] = {
-    {32, 128, 4, 0.375, 4.1, 530}, {32, 256, 2, 0.40, 5.9, 350}, {64, 128, 3, 0.45, 4.5, 560},
-    {64, 256, 2, 1.12, 6.2, 660}, {128, 128, 2, 0.385, 5.9, 940}, {256, 256, 1, 1.31, 14.9, 1460}};
+    {32, 128, 4, 0.43, 3.4, 434}, {32, 256, 2, 0.96, 3.3, 366}, {64, 128, 3, 0.57, 3.8, 500},
+    {64, 256, 2, 0.526, 8.0, 576}, {128, 128, 2, 0.69, 5.3, 667}, {256, 256, 1, 1.15, 13.3, 1108}};
 constexpr int kLinearTileCount = sizeof(kLinearTiles) / sizeof(kLinearTiles[0]);
 struct LinearPlan { int tile, splits; };        // tile -1: linear_rows_kernel
 
@@ -560,9 +560,9 @@ static LinearPlan plan_linear(int64_t m, int64_t n, int64_t k) {
             const double compute = std::ceil(groups / 256) * per * (2.0 * l.bm * l.bn * 64) / (l.tflops * 1e6 / 256);
             const double rounds = groups / (256.0 * l.resident), wait = std::ceil(rounds) * per * l.block_us;
             // weights, x and the result from and to memory, slower from few workgroups; what all tiles load, through the L2s
-            const double spread = groups < 384 ? 1.0 + (384 - groups) / 1385 : 1.0;
-            const double memory = (2.0 * ((double)n * k + (double)m * k) * spread + 3.4 * (double)m * n) / 8.1e6 + 2.0 * tiles * (l.bm + l.bn) * k / 3.8e7;
-            const double join = splits > 1 ? 2.65 + (double)splits * m * n * 8 / 5.3e6 : 0.0;
+            const double spread = groups < 384 ? 1.0 + (384 - groups) / 1230 : 1.0;
+            const double memory = (2.0 * ((double)n * k + (double)m * k) * spread + 3.1 * (double)m * n) / 4.55e6 + 2.0 * tiles * (l.bm + l.bn) * k / 2.46e7;
+            const double join = splits > 1 ? 3.8 + (double)splits * m * n * 8 / 6.7e6 : 0.0;
             const double us = std::max(std::max(compute, wait), memory) + std::max(rounds, 1.0) * l.tile_us + join;
             if (us < least) { least = us; best = {t, splits}; }
         }
