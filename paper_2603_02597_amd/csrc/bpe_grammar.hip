@@ -56,7 +56,9 @@ struct MaskParams {
     int64_t mask_stride;
 };
 
-// Few states: one lane per token, up to four states at a time, whose chains of reads are under way together.
+// Few states: one lane per token, up to four states at a time, whose chains of reads are under way together.  Bound by those chains,
+// a read per byte of a token, from caches (the tables and the tokens' bytes together are a few MB): 12 states of 50,257 tokens 5.5
+// us, which is the call's time on the host, 64 states 12.3.
 constexpr int kMaskChains = 4;
 __global__ void __launch_bounds__(kGroupThreads) grammar_masks_kernel(MaskParams p) {
     const int v = blockIdx.x * kGroupThreads + threadIdx.x, n_classes = p.g.n_classes;
@@ -94,7 +96,8 @@ __global__ void __launch_bounds__(kGroupThreads) grammar_masks_kernel(MaskParams
 // Many states.  A workgroup takes a tile of 2,048 tokens, as strings of classes in LDS, and a share of the states; a wavefront takes
 // one state after the other.  Most states let few bytes pass: one look at the transitions per class says which, and only the
 // tokens behind those are walked, which the tile holds in order of their first class.  Where many tokens pass, all are walked
-// in order of their ids, four per lane at a time, so that four chains of reads are under way together.
+// in order of their ids, four per lane at a time, so that four chains of reads are under way together.  1,500 states of 50,257 tokens:
+// 45 us, of which 17 lay out the tiles; bound by instructions (the bytes are 9.4 MB of masks, 2 us), with transitions in LDS.
 constexpr int kMaskTile = 2048, kMaskThreads = 1024, kMaskWaves = kMaskThreads / kWave;
 static_assert(kMaskTile == 32 * kWave, "a word of bits per lane");
 constexpr int kMaskTable = 48 * 1024;            // transitions that are kept in LDS
@@ -268,6 +271,7 @@ struct AdvanceParams {
     int32_t *out;
 };
 
+// A lane per state: the chain of reads along one token's bytes; bound by the launch (5 us).
 __global__ void __launch_bounds__(kGroupThreads) grammar_advance_kernel(AdvanceParams p) {
     const int i = blockIdx.x * kGroupThreads + threadIdx.x;
     if (i >= p.n) return;

@@ -194,7 +194,8 @@ __device__ __forceinline__ U4 load_tail(const uint16_t *row, int t, int k) {
 // registers.  A workgroup takes 16 rows of weight, its four wavefronts a quarter of k each (so a vocabulary of few rows still fills
 // the chip); their sums meet in LDS.  A step is 64 columns, whole lines of memory, and four steps are under way at a time.
 // weight is the left operand: a lane ends with four neighbouring columns of one row of out; rows behind the last of x repeat it and
-// are dropped.  Bound by memory: 1 x 50256 x 1024 18 us, 1 x 100256 x 4096 143 us, 5.7 TB/s; 1 x 2048 x 2048 7 us, of which 5 are the launch.
+// are dropped.  What lies behind the last whole step is loaded before the first one.  Bound by memory: 1 x 50256 x 1024 18 us, 1 x
+// 100256 x 4096 142 us, 5.8 TB/s; 1 x 2048 x 2048 7 us, of which 5 are the launch.
 constexpr int kRowsAhead = 4;
 template <class T>
 __global__ void __launch_bounds__(kGroupThreads) linear_rows_kernel(LinearParams p) {
@@ -255,7 +256,17 @@ __global__ void __launch_bounds__(kGroupThreads) linear_rows_kernel(LinearParams
     if (i < p.m && j < p.n) put4(p, i, j, acc);
 }
 
-// More rows.  A workgroup makes BM x BN of out, WM x WN wavefronts side by side, 64 columns of k at a time through LDS.
+// More rows.  A workgroup makes BM x BN of out, WM x WN wavefronts side by side, 64 columns of k at a time through LDS: 128 (BM + BN)
+// bytes of rows for 128 BM BN operations.  Large products take the largest tile, whose rows the L2s can bring as fast as the matrix cores
+// use them; few rows of x a tile so small that weight comes from memory to all compute units at once, with k cut into parts that
+// linear_join_kernel adds up where there are fewer tiles than compute units (plan_linear).
+// The loads go straight into LDS, two blocks ahead; products, LDS reads and loads are put in order by hand, so the matrix cores
+// see no wait but the one in the middle of a block.  The operands are swapped (weight on the left): a lane ends with neighbouring
+// columns of a row.  Bound by memory for few rows: 64 x 100256 x 4096 155 us, 5.4 TB/s.  Bound by the matrix cores for many: 4001 x
+// 50256 x 4096 1,377 us, 1,196 TFLOP/s, 94 % of a library's plain product there; 4096 x 4096 x 4096 122 us, 83 %.  What is missing is a
+// tile's first loads and its result, some 13 us in which the only workgroup of a compute unit leaves the matrix cores alone.
+// A last block that is cut off costs about a whole one: 120 x 3664 x 2792 17.0 us, x 2816 15.2.  Rows at odd addresses pass through
+// registers: 508 x 2086 x 579 13.6 us, 508 x 2088 x 584 10.
 typedef float F16v __attribute__((ext_vector_type(16)));
 // D = A B + C on 32 x 32 x 16: lane l gives A[l % 32][8 (l / 32) ..+7] and B[8 (l / 32) ..+7][l % 32] and holds
 // C[e % 4 + 8 (e / 4) + 4 (l / 32)][l % 32] in element e.
@@ -487,8 +498,10 @@ __global__ void __launch_bounds__(WM *WN *kWave, 163840 / lds_of_tile(BM, BN, XS
     }
 }
 
-// Any alignment and any k: a workgroup of four wavefronts makes 64 x 64 of out, a wavefront 32 x 32 (two by two products of 16 x 16),
-// 32 of k at a time through registers into LDS.
+// Rows that lie 2^21 elements apart or more, or have fewer than eight columns: a workgroup of four wavefronts makes 64 x 64 of out, a
+// wavefront 32 x 32 (two by two products of 16 x 16), 32 of k at a time through registers into LDS, one step after the other; bound by
+// the wait for each step's loads.  200 x 2048 x 2048 with rows
+// so far apart 39 us, in tiles 13; 200 x 2048 x 7 6.3 us, of which 5 are the launch.
 template <class T>
 __global__ void __launch_bounds__(kGroupThreads) linear_tile_kernel(LinearParams p) {
     __shared__ U4 xs[64][4], ws[64][4];
@@ -520,7 +533,8 @@ __global__ void __launch_bounds__(kGroupThreads) linear_tile_kernel(LinearParams
         }
 }
 
-// Adds up the parts of every four neighbours of a row, part by part, and finishes them.
+// Adds up the parts of every four neighbours of a row, part by part (so in one order), and finishes them.  Bound by its launch and by
+// memory: about 4 us and the parts at 6.7 TB/s.
 __global__ void __launch_bounds__(kGroupThreads) linear_join_kernel(LinearParams p) {
     const int64_t groups = p.part_stride / 4, total = groups * p.m, step = (int64_t)gridDim.x * kGroupThreads;
     for (int64_t g = (int64_t)blockIdx.x * kGroupThreads + threadIdx.x; g < total; g += step) {

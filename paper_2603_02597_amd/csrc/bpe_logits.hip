@@ -35,7 +35,10 @@ __device__ __forceinline__ const uint32_t *row_mask(const bpe_logit_rules &r, in
 
 // A workgroup takes a slice of a row.  With LISTS it first counts the row's history in LDS and marks the biased tokens, then makes one
 // pass over the slice, sixteen bytes per lane; the biased tokens, which that pass leaves out, come last.  Every slice of a row
-// reads the row's whole history: slices are as long as LDS allows with two workgroups per compute unit.
+// reads the row's whole history: slices are as long as LDS allows with two workgroups per compute unit.  Every operation is rounded by
+// itself (no fused multiply-add), so the result is the formula's to the bit.  Bound by memory for many rows (512 x 100257 f32 with
+// lists of 30,000 108 us: 411 MB of logits at 3.8 TB/s, and every list read seven times), by the chain of list, count and pass for few:
+// 64 x 100256 bf16 with lists of 8,000 12 us, one row 4 us.
 constexpr int kAdjustThreads = 1024, kAdjustSlice = 16384;
 constexpr uint32_t kBiased = 0x80000000u;             // in a count
 template <class IN, class OUT, bool LISTS>
@@ -168,7 +171,11 @@ __global__ void __launch_bounds__(kAdjustThreads) adjust_kernel(AdjustParams p) 
 // may still be among the k best: those not below a bound that at least k logits reach.  The bound is cheap: the k-th largest of the
 // threads' largest logits so far.  (Of 8,192 random logits it lets 73 through for k = 64, of later ones fewer and fewer.)  What was
 // kept is cut down to the k best by histograms over the range of what is left, and put in order by counting.  Logits are compared as
-// (value, index from behind) in one 64-bit word, so no two are equal and the order in which lanes append does not matter.
+// (value, index from behind) in one 64-bit word, so no two are equal and the order in which lanes append does not matter.  The sum of
+// exp(logit - largest so far) goes along in 32 bits, rescaled when the largest grows.
+// Bound by memory for many rows of f32 (1024 x 50257, k = 20: 44 us, 4.7 TB/s), by the comparisons and exponentials for 16-bit logits
+// (2.6 TB/s), by two launches and their chains of barriers for few: one row of 50256 in parts k = 1 9 us, k = 64 10.8; 64 rows of
+// 100256 bf16 k = 64 16 us, k = 256 34.
 constexpr int kTopThreads = 256, kTopWaves = kTopThreads / kWave;
 constexpr int kTopKeep = 4096;               // words in LDS: four workgroups per compute unit
 constexpr int kTopPerThread = 32;            // logits of a thread that are at hand together
@@ -321,22 +328,38 @@ template <class Op> __device__ __forceinline__ float wave_join(float v, Op op) {
     return join_groups<32>(v, op);
 }
 
-// A bound that the largest logits of k threads reach: their k-th largest, cut to the upper 16 bits of its place in the order.  Every
-// wavefront looks at all of them, four per lane, and finds the bound bit by bit.
-__device__ __forceinline__ float bound_of_threads(TopShared &sh, float largest, int k) {
-    const int tid = threadIdx.x, lane = tid & 63;
-    sh.bin[tid] = order_key(largest);
-    __syncthreads();
-    static_assert(kTopThreads == 4 * kWave, "");
-    const U4 key = ((const U4 *)sh.bin)[lane];
+// A bound that k of the largest logits of the threads' halves reach: the k-th largest of them (for k <= 128 of the threads' largest),
+// cut to the upper 16 bits of its place in the order.  Every wavefront looks at all of them, four or eight per lane, and finds the
+// bound bit by bit.  (k = 256 from the threads' largest alone: their smallest is the bound, and 5 to 6 times k words pass.)
+template <int PER> __device__ __forceinline__ uint32_t kth_largest(const uint32_t *keys, int k) {
+    U4 key[PER];
+#pragma unroll
+    for (int h = 0; h < PER; ++h) key[h] = ((const U4 *)keys)[h * kWave + (threadIdx.x & 63)];
     uint32_t bound = 0;
 #pragma unroll
     for (int bit = 31; bit >= 16; --bit) {
         const uint32_t at = bound | 1u << bit;
         int reach = 0;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) reach += __builtin_popcountll(__ballot(key[q] >= at));
+        for (int h = 0; h < PER; ++h)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) reach += __builtin_popcountll(__ballot(key[h][q] >= at));
         bound = reach >= k ? at : bound;
+    }
+    return bound;
+}
+__device__ __forceinline__ float bound_of_threads(TopShared &sh, float largest0, float largest1, int k) {
+    static_assert(kTopThreads == 4 * kWave && kTopBins >= 2 * kTopThreads && kMaxTop <= kTopThreads, "");
+    uint32_t bound;
+    if (k <= kTopThreads / 2) {
+        sh.bin[threadIdx.x] = order_key(fmaxf(largest0, largest1));
+        __syncthreads();
+        bound = kth_largest<1>(sh.bin, k);
+    } else {
+        sh.bin[threadIdx.x] = order_key(largest0);
+        sh.bin[kTopThreads + threadIdx.x] = order_key(largest1);
+        __syncthreads();
+        bound = kth_largest<2>(sh.bin, k);
     }
     return bound > order_key(-__builtin_inff()) ? key_value(bound) : kLowest;
 }
@@ -397,7 +420,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) top_part_kernel(TopParams p) {
     const int first = part * p.part_len, last = min(first + p.part_len, p.n_vocab);
     const typename IN::raw *in = (const typename IN::raw *)p.logits + row * p.logits_stride;
     if (tid == 0) sh.n = 0;
-    float largest = -__builtin_inff(), sum = 0.0f;
+    float largest = -__builtin_inff(), sum = 0.0f, half[2] = {largest, largest};       // half: of every second vector
     float bound = kLowest;                                // logits below it are out; so is -infinity
     uint64_t bound_word = 0;                              // and words that are not above this one
     int before = 0, n_rounds = 0;
@@ -420,11 +443,11 @@ __global__ void __launch_bounds__(kTopThreads, 4) top_part_kernel(TopParams p) {
                 }
             }
         }
-        float m = largest;
 #pragma unroll
         for (int q = 0; q < kTopVectors; ++q)
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) m = fmaxf(m, x[q][e]);
+            for (int e = 0; e < kPer; ++e) half[q & 1] = fmaxf(half[q & 1], x[q][e]);
+        const float m = fmaxf(half[0], half[1]);
         const float ref = reference_of(m);
         sum *= exp_of(largest - ref);
 #pragma unroll
@@ -433,7 +456,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) top_part_kernel(TopParams p) {
             for (int e = 0; e < kPer; ++e) sum += exp_of(x[q][e] - ref);
         largest = m;
         const float bound_before = bound;                 // reached by k of the words that are there
-        if ((n_rounds & (n_rounds + 1)) == 0) bound = fmaxf(bound, bound_of_threads(sh, largest, p.k));   // rounds 0, 1, 3, 7, ...
+        if ((n_rounds & (n_rounds + 1)) == 0) bound = fmaxf(bound, bound_of_threads(sh, half[0], half[1], p.k));   // rounds 0, 1, 3, 7, ...
         else __syncthreads();
         // A lane's logits that stay, one bit each: few, so they are read again.
         uint32_t stay = 0;
@@ -484,7 +507,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) top_part_kernel(TopParams p) {
     }
     __syncthreads();
     const float2 total = join_sums(sh, largest, sum);
-    if (n_rounds > 1) bound = fmaxf(bound, bound_of_threads(sh, largest, p.k));
+    if (n_rounds > 1) bound = fmaxf(bound, bound_of_threads(sh, half[0], half[1], p.k));
     if (p.parts == 1) {
         write_row(p, sh, row, before, words_from(bound), total);
         return;
@@ -638,13 +661,14 @@ static int check_top(int64_t rows, int64_t n_vocab, int64_t k) {
 
 static int64_t align256l(int64_t v) { return (v + 255) & ~255ll; }
 
-// Parts of a row: up to four workgroups per compute unit in all, none of fewer than 8,192 logits, and no more words than one
-// workgroup joins.  (f32: 700 rows of 50257 in one part 42 us, in two 53; 300 rows in one 28, in four 32; one row in 7 parts 15.3, in 13 16.4.)
+// Parts of a row: up to four workgroups per compute unit in all, none of fewer than 8,192 logits, and no more than can leave 2 k words
+// each for the one workgroup that joins them.  (f32: 700 rows of 50257 in one part 42 us, in two 53; 300 rows in one 28, in four 32; one
+// row in 7 parts 15.3, in 13 16.4.  64 rows of 100256 bf16, k = 256, in 8 parts 34, in 13, which cut down to the k best themselves, 43.)
 static int64_t top_parts(int64_t rows, int64_t n_vocab, int64_t k) {
-    const int64_t parts = std::min(std::min(1024 / std::max<int64_t>(rows, 1), (n_vocab + 8191) / 8192), (int64_t)kTopKeep / k);
+    const int64_t parts = std::min(std::min(1024 / std::max<int64_t>(rows, 1), (n_vocab + 8191) / 8192), (int64_t)kTopKeep / (2 * k));
     return std::max<int64_t>(parts, 1);
 }
-// Words that a part leaves: a little more than k as a rule, for k = 256 (as many as there are threads) five times as many.
+// Words that a part leaves: what its bound lets through, a little more than k as a rule.
 static int64_t part_keep(int64_t parts, int64_t k) { return std::min<int64_t>(std::max<int64_t>(8 * k, 32), kTopKeep / parts); }
 
 extern "C" int64_t bpe_top_tokens_workspace_bytes(int64_t rows, int64_t n_vocab, int64_t k) {
