@@ -36,23 +36,26 @@ template <> __device__ __forceinline__ F4 mma16<F16>(U4 a, U4 b, F4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(F16x8, a), __builtin_bit_cast(F16x8, b), c, 0, 0, 0);
 }
 
-// The activations without a branch, from the hardware's 2^x and reciprocal (a unit in the last place each); where the factor of v
-// is 0 they give their limit, 0, for -infinity too.
-__device__ __forceinline__ float scaled(float v, float factor) { return factor == 0.0f ? 0.0f : v * factor; }
-__device__ __forceinline__ float sigmoid_of(float minus_log2_odds) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(minus_log2_odds)); }
+// The activations without a branch, from the hardware's 2^x and reciprocal (a unit in the last place each).  A factor of 0 meets the largest
+// finite value in place of an infinity, so that all give their limits; a NaN stays one through the factor.
+constexpr float kMost = 3.402823466e38f, kLog2Of = 1.44269504088896341f;
 __device__ __forceinline__ float relu(float v) { return v < 0.0f ? 0.0f : v; }
+__device__ __forceinline__ float times_sigmoid(float v, float minus_log2_odds) {
+    return fmaxf(v, -kMost) * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(minus_log2_odds));
+}
 // v (1 + erf(v / sqrt 2)) / 2 = max(v, 0) - |v| q with q = (1 - erf(|v| / sqrt 2)) / 2, by the approximation 7.1.26 of Abramowitz and
-// Stegun's handbook, which is good to 1.5e-7 of 1.
+// Stegun's handbook, which is good to 1.5e-7 of 1 (its coefficients by 1 / 2, its p by 1 / sqrt 2).
 __device__ __forceinline__ float gelu(float v) {
-    const float z = __builtin_fabsf(v) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * z);
-    const float series = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
-    return relu(v) - scaled(__builtin_fabsf(v), 0.5f * series * __builtin_amdgcn_exp2f(-1.44269504088896341f * z * z));
+    const float size = __builtin_fabsf(v), t = __builtin_amdgcn_rcpf(1.0f + (0.3275911f * 0.70710678118654752f) * size);
+    const float series = t * (0.127414796f + t * (-0.142248368f + t * (0.7107068705f + t * (-0.7265760135f + t * 0.5307027145f))));
+    return fmaxf(v, 0.0f) - fminf(size, kMost) * (series * __builtin_amdgcn_exp2f(v * v * (-0.5f * kLog2Of)));
 }
-// v (1 + tanh u) / 2 = v / (1 + exp(-2 u))
+// v (1 + tanh u) / 2 = v / (1 + exp(-2 u)), u = sqrt(2 / pi) (v + 0.044715 v^3)
 __device__ __forceinline__ float gelu_tanh(float v) {
-    return scaled(v, sigmoid_of(-2.0f * 1.44269504088896341f * 0.79788456080286536f * (v + 0.044715f * v * v * v)));
+    constexpr float c = -2.0f * kLog2Of * 0.79788456080286536f;
+    return times_sigmoid(v, v * (c + (c * 0.044715f) * (v * v)));
 }
-__device__ __forceinline__ float silu(float v) { return scaled(v, sigmoid_of(-1.44269504088896341f * v)); }
+__device__ __forceinline__ float silu(float v) { return times_sigmoid(v, v * -kLog2Of); }
 
 template <int ROWS> __device__ __forceinline__ void activate(F4 (&v)[ROWS], int activation) {
 #define EACH(FUNCTION) \
@@ -106,54 +109,94 @@ template <int ROWS> __device__ __forceinline__ void fetch(const LinearParams &p,
         }
     }
 }
-// The epilogue of these columns, as far as they exist, of these rows, as far as they do; `bias`: of bias_of, `res`: of fetch.
-// (Every lane of a call takes the same branches but those at the edges.)
-template <int ROWS>
-__device__ __forceinline__ void put(const LinearParams &p, int i, int step, int j, F4 (&v)[ROWS], F4 bias, const U4 (&res)[ROWS]) {
+// Bias (of bias_of), activation and residual (of fetch).
+template <int ROWS> __device__ __forceinline__ void finish(const LinearParams &p, F4 (&v)[ROWS], F4 bias, const U4 (&res)[ROWS]) {
     if (p.bias) {
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) v[u] += bias;
     }
     activate(v, p.activation);
-    if (j + 3 >= p.n) {
+    if (!p.residual) return;
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u) {
+        if (p.out_dtype == BPE_F32) {
+            v[u] += __builtin_bit_cast(F4, res[u]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[u][e] += out_to_float(p, (uint16_t)(res[u][e / 2] >> 16 * (e % 2)));
+        }
+    }
+}
+__device__ __forceinline__ H4Any narrow(const LinearParams &p, F4 v) {
+    H4Any o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = out_from_float(p, v[e]);
+    return o;
+}
+// The epilogue of these columns, as far as they exist, of these rows, as far as they do.
+template <int ROWS>
+__device__ __forceinline__ void put(const LinearParams &p, int i, int step, int j, F4 (&v)[ROWS], F4 bias, U4 (&res)[ROWS]) {
+    if (p.residual && j + 3 >= p.n) {
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) {
-            const int64_t row = i + u * step;
+            const int64_t from = min(i + u * step, p.m - 1) * p.residual_stride + j;
+            res[u] = U4{0, 0, 0, 0};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if (row >= p.m || j + e >= p.n) break;
-                float x = v[u][e];
-                if (p.residual) x += load_as_float(p.residual, row * p.residual_stride + j + e, p.out_dtype);
-                const int64_t at = row * p.out_stride + j + e;
-                if (p.out_dtype == BPE_F32) ((float *)p.out)[at] = x;
-                else ((uint16_t *)p.out)[at] = out_from_float(p, x);
-            }
-        }
-        return;
-    }
-    if (p.residual) {
-#pragma unroll
-        for (int u = 0; u < ROWS; ++u) {
-            if (p.out_dtype == BPE_F32) {
-                v[u] += __builtin_bit_cast(F4, res[u]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[u][e] += out_to_float(p, (uint16_t)(res[u][e / 2] >> 16 * (e % 2)));
+                if (j + e >= p.n) break;
+                if (p.out_dtype == BPE_F32) res[u][e] = ((const uint32_t *)p.residual)[from + e];
+                else res[u][e / 2] |= (uint32_t)((const uint16_t *)p.residual)[from + e] << 16 * (e % 2);
             }
         }
     }
+    finish(p, v, bias, res);
 #pragma unroll
     for (int u = 0; u < ROWS; ++u) {
         const int64_t row = i + u * step, at = row * p.out_stride + j;
         if (row >= p.m) break;
-        if (p.out_dtype == BPE_F32) {
+        if (j + 3 >= p.n) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (j + e >= p.n) break;
+                if (p.out_dtype == BPE_F32) ((float *)p.out)[at + e] = v[u][e];
+                else ((uint16_t *)p.out)[at + e] = out_from_float(p, v[u][e]);
+            }
+        } else if (p.out_dtype == BPE_F32) {
             *(F4Any *)((float *)p.out + at) = v[u];
         } else {
-            H4Any o;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = out_from_float(p, v[u][e]);
-            *(H4Any *)((uint16_t *)p.out + at) = o;
+            *(H4Any *)((uint16_t *)p.out + at) = narrow(p, v[u]);
         }
+    }
+}
+// The same two for a tile that lies within out as a whole: `row` and the tile's first column `col` are the same in all lanes, which are
+// `lane_at` bytes from there, so that addresses cost the vector unit nothing.
+template <int ROWS> __device__ __forceinline__ void fetch_whole(const LinearParams &p, int row, int step, int col, uint32_t lane_at, U4 (&res)[ROWS]) {
+    if (!p.residual) return;
+    typedef uint32_t U2Any __attribute__((ext_vector_type(2), aligned(2)));
+    if (p.out_dtype == BPE_F32) {
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) {
+            const char *from = (const char *)((const float *)p.residual + (row + u * step) * p.residual_stride + col);
+            res[u] = __builtin_bit_cast(U4, *(const F4Any *)(from + lane_at));
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) {
+            const char *from = (const char *)((const uint16_t *)p.residual + (row + u * step) * p.residual_stride + col);
+            const U2Any r = *(const U2Any *)(from + lane_at);
+            res[u] = U4{r[0], r[1], 0, 0};
+        }
+    }
+}
+template <int ROWS>
+__device__ __forceinline__ void put_whole(const LinearParams &p, int row, int step, int col, uint32_t lane_at, F4 (&v)[ROWS], F4 bias, const U4 (&res)[ROWS]) {
+    finish(p, v, bias, res);
+    if (p.out_dtype == BPE_F32) {
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) *(F4Any *)((char *)((float *)p.out + (row + u * step) * p.out_stride + col) + lane_at) = v[u];
+    } else {
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) *(H4Any *)((char *)((uint16_t *)p.out + (row + u * step) * p.out_stride + col) + lane_at) = narrow(p, v[u]);
     }
 }
 __device__ __forceinline__ void put4(const LinearParams &p, int i, int j, F4 v) {
@@ -263,8 +306,8 @@ __global__ void __launch_bounds__(kGroupThreads) linear_rows_kernel(LinearParams
 // The loads go straight into LDS, two blocks ahead; products, LDS reads and loads are put in order by hand, so the matrix cores
 // see no wait but the one in the middle of a block.  The operands are swapped (weight on the left): a lane ends with neighbouring
 // columns of a row.  Bound by memory for few rows: 64 x 100256 x 4096 155 us, 5.4 TB/s.  Bound by the matrix cores for many: 4001 x
-// 50256 x 4096 1,377 us, 1,196 TFLOP/s, 94 % of a library's plain product there; 4096 x 4096 x 4096 122 us, 83 %.  What is missing is a
-// tile's first loads and its result, some 13 us in which the only workgroup of a compute unit leaves the matrix cores alone.
+// 50256 x 4096 1,356 us, 1,215 TFLOP/s, 95 % of a library's plain product there; 4096 x 4096 x 4096 119 us, 87 %.  What is missing is a
+// tile's first loads and its result, some 10 us in which the only workgroup of a compute unit leaves the matrix cores alone.
 // A last block that is cut off costs about a whole one: 120 x 3664 x 2792 17.0 us, x 2816 15.2.  Rows at odd addresses pass through
 // registers: 508 x 2086 x 579 13.6 us, 508 x 2088 x 584 10.
 typedef float F16v __attribute__((ext_vector_type(16)));
@@ -291,15 +334,19 @@ template <int LATER> __device__ __forceinline__ void wait_and_meet() {
 
 // Which tile of out a workgroup makes.  Workgroups go round the eight chiplets by their index, and each chiplet has an L2 of its
 // own: so every chiplet gets a run of neighbouring tiles, eight rows of tiles by as many columns as it takes.
-__device__ __forceinline__ bool tile_of(int64_t tiles_m, int64_t tiles_n, int splits, int64_t &tm, int64_t &tn, int &split) {
-    const int64_t tiles = tiles_m * tiles_n, total = tiles * splits, per = (total + 7) / 8;
-    int64_t s = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if ((int64_t)(blockIdx.x >> 3) >= per || s >= total) return false;
-    split = (int)(s / tiles);
-    s %= tiles;
-    const int64_t group = s / (8 * tiles_n), rest = s % (8 * tiles_n), high = min<int64_t>(8, tiles_m - 8 * group);
-    tm = 8 * group + rest % high;
-    tn = rest / high;
+// (In 32 bits: a launch has fewer than 2^24 workgroups, and a division of 64 bits takes a fifth of a microsecond.)
+__device__ __forceinline__ bool tile_of(uint32_t tiles_m, uint32_t tiles_n, uint32_t splits, int &tm, int &tn, int &split) {
+    const uint32_t tiles = tiles_m * tiles_n, total = tiles * splits, per = (total + 7) / 8;
+    uint32_t s = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if ((blockIdx.x >> 3) >= per || s >= total) return false;
+    split = 0;
+    if (splits > 1) {
+        split = (int)(s / tiles);
+        s -= split * tiles;
+    }
+    const uint32_t group = s / (8 * tiles_n), rest = s - group * (8 * tiles_n), high = min(8u, tiles_m - 8 * group);
+    tn = (int)(high == 8 ? rest / 8 : rest / high);
+    tm = (int)(8 * group + rest - tn * high);
     return true;
 }
 static int64_t tile_grid(int64_t tiles_m, int64_t tiles_n, int splits) { return (tiles_m * tiles_n * splits + 7) / 8 * 8; }
@@ -314,15 +361,19 @@ __global__ void __launch_bounds__(WM *WN *kWave, 163840 / lds_of_tile(BM, BN, XS
     constexpr int kX = BM * 128, kW = BN * 128;                        // bytes of a block's rows of x and of weight: XS and two of them
     __shared__ __attribute__((aligned(1024))) char lds[lds_of_tile(BM, BN, XS)];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int64_t tile_m, tile_n;
-    int split;
+    int tile_m, tile_n, split;
     if (!tile_of((p.m + BM - 1) / BM, (p.n + BN - 1) / BN, p.splits, tile_m, tile_n, split)) return;
-    const int i0 = (int)tile_m * BM, j0 = (int)tile_n * BN;
+    const int i0 = tile_m * BM, j0 = tile_n * BN;
     // Sixteen-byte groups of a row lie in LDS at their index XOR the row's last three bits, so that eight neighbouring rows
     // read at one index meet eight different groups of banks.
     const int row8 = lane >> 3, group = (lane & 7) ^ row8;
     // this part's blocks of 64 columns; the last one of all may be cut off
-    const int all_blocks = (p.k + 63) >> 6, block0 = (int)((int64_t)all_blocks * split / p.splits), blocks = (int)((int64_t)all_blocks * (split + 1) / p.splits) - block0;
+    const uint32_t all_blocks = (uint32_t)(p.k + 63) >> 6;
+    int block0 = 0, blocks = (int)all_blocks;
+    if (p.splits > 1) {
+        block0 = (int)(all_blocks * (uint32_t)split / (uint32_t)p.splits);
+        blocks = (int)(all_blocks * (uint32_t)(split + 1) / (uint32_t)p.splits) - block0;
+    }
     const int cut = split == p.splits - 1 ? p.k & 63 : 0;             // the columns of a last block that is cut off, or 0
     // Columns of this lane's group of a cut block that lie behind the row's end, or behind its last whole group where rows are aligned:
     // the group is loaded from so much further in front (eight columns in front of the block at most, and k >= 8) and mended in LDS.
@@ -450,19 +501,28 @@ __global__ void __launch_bounds__(WM *WN *kWave, 163840 / lds_of_tile(BM, BN, XS
     }
     // The result goes through LDS, 32 rows of a wavefront's part at a time, so that a row's columns leave next to each other:
     // the lanes hold one row each, four columns at a time.  (The padding of four columns spreads the rows over the banks.)
+    // A batch of rows at a time: their reads and their stores are under way together, and so is the residual of the next batch (but in
+    // the smallest tiles, which have few registers and other workgroups beside them).
     constexpr int kCols = 32 * TN, kPitch = kCols + 4, kLanesPerRow = kCols / 4;
-    static_assert(NW * 32 * kPitch * 4 <= XS * kX + 2 * kW, "the rows of all wavefronts fit the buffers");
-    float *stage = (float *)lds + wv * (32 * kPitch);
-    // a batch of rows at a time: their reads and their stores are under way together, and so is the residual of the next batch
-    constexpr int kStep = 64 / kLanesPerRow, kBatch = kStep < 4 ? 8 : 4, kRows = kBatch * kStep;
+    constexpr int kStep = 64 / kLanesPerRow, kBatch = kStep >= 4 ? 4 : 8, kRows = kBatch * kStep;
     const int j = j0 + wn * kCols + 4 * (lane % kLanesPerRow), i = i0 + wm * (BM / WM) + lane / kLanesPerRow;
-    const float *mine = stage + lane / kLanesPerRow * kPitch + 4 * (lane % kLanesPerRow);
-    U4 res[kBatch], next[kBatch];
+    const int top = i0 + wm * (BM / WM), left = j0 + wn * kCols;                       // of this wavefront
+    const bool whole = i0 + BM <= p.m && j0 + BN <= p.n;
+    const uint32_t size = p.out_dtype == BPE_F32 ? 4 : 2, column_at = 4u * (lane % kLanesPerRow);
+    const uint32_t out_at = size * ((uint32_t)(lane / kLanesPerRow) * (uint32_t)p.out_stride + column_at);
+    const uint32_t res_at = size * ((uint32_t)(lane / kLanesPerRow) * (uint32_t)p.residual_stride + column_at);
+    const uint32_t part_at = 4 * ((uint32_t)(lane / kLanesPerRow) * (uint32_t)p.part_stride + column_at);
+    constexpr bool kAhead = kStep < 8;
+    U4 res[kBatch], next[kAhead ? kBatch : 1];
     F4 bias = {0, 0, 0, 0};
     if (p.splits == 1) {
         bias = bias_of(p, j);
-        fetch(p, i, kStep, j, next);
+        if (kAhead && whole) fetch_whole(p, top, kStep, left, res_at, next);
+        else if (kAhead) fetch(p, i, kStep, j, next);
     }
+    static_assert(NW * 32 * kPitch * 4 <= XS * kX + 2 * kW, "the rows of all wavefronts fit the buffers");
+    float *stage = (float *)lds + wv * (32 * kPitch);
+    const float *mine = stage + lane / kLanesPerRow * kPitch + 4 * (lane % kLanesPerRow);
 #pragma unroll 1
     for (int a = 0; a < TM; ++a) {
 #pragma unroll
@@ -481,16 +541,33 @@ __global__ void __launch_bounds__(WM *WN *kWave, 163840 / lds_of_tile(BM, BN, XS
             F4 v[kBatch];
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) v[u] = *(const F4 *)(mine + (r + u * kStep) * kPitch);
-            if (j >= p.n) continue;
             const int row = i + 32 * a + r;
+            if (p.splits == 1 && whole) {
+                if constexpr (kAhead) {
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u) res[u] = next[u];
+                    if (32 * a + r + kRows < BM / WM) fetch_whole(p, top + 32 * a + r + kRows, kStep, left, res_at, next);
+                } else {
+                    fetch_whole(p, top + 32 * a + r, kStep, left, res_at, res);
+                }
+                put_whole(p, top + 32 * a + r, kStep, left, out_at, v, bias, res);
+                continue;
+            }
+            if (j >= p.n) continue;
             if (p.splits > 1) {
 #pragma unroll
-                for (int u = 0; u < kBatch; ++u)
-                    if (row + u * kStep < p.m) *(F4 *)(p.part + ((int64_t)split * p.m + row + u * kStep) * p.part_stride + j) = v[u];
+                for (int u = 0; u < kBatch; ++u) {                  // (so few tiles that the lanes' offsets fit 32 bits)
+                    char *to = (char *)(p.part + ((int64_t)split * p.m + top + 32 * a + r + u * kStep) * p.part_stride + left);
+                    if (whole || row + u * kStep < p.m) *(F4 *)(to + part_at) = v[u];
+                }
             } else {
+                if constexpr (kAhead) {
 #pragma unroll
-                for (int u = 0; u < kBatch; ++u) res[u] = next[u];
-                fetch(p, row + kRows, kStep, j, next);
+                    for (int u = 0; u < kBatch; ++u) res[u] = next[u];
+                    fetch(p, row + kRows, kStep, j, next);
+                } else {
+                    fetch(p, row, kStep, j, res);
+                }
                 put(p, row, kStep, j, v, bias, res);
             }
         }
@@ -506,10 +583,9 @@ template <class T>
 __global__ void __launch_bounds__(kGroupThreads) linear_tile_kernel(LinearParams p) {
     __shared__ U4 xs[64][4], ws[64][4];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    int64_t tile_m, tile_n;
-    int split;
+    int tile_m, tile_n, split;
     if (!tile_of((p.m + 63) / 64, (p.n + 63) / 64, 1, tile_m, tile_n, split)) return;
-    const int i0 = (int)tile_m * 64, j0 = (int)tile_n * 64;
+    const int i0 = tile_m * 64, j0 = tile_n * 64;
     const int wi = 32 * (wv >> 1), wj = 32 * (wv & 1);
     const uint16_t *xr = p.x + min(i0 + (tid >> 2), p.m - 1) * p.x_stride, *wr = p.w + min(j0 + (tid >> 2), p.n - 1) * p.w_stride;
     F4 acc[2][2] = {};
@@ -550,7 +626,7 @@ __global__ void __launch_bounds__(kGroupThreads) linear_join_kernel(LinearParams
 // row: its sides, how many of its workgroups a compute unit holds, us for a block of 64 columns when a workgroup waits for
 // its loads alone, us for its first loads and its result, and the TFLOP/s of the whole chip when nothing else bounds it.  The
 // numbers are fitted to the times of all tiles and parts on 93 sizes (m 5 to 8192, n 256 to 128000, k 64 to 4096); there the choice takes
-// 1.6 % longer than the best one on average, 19 % at worst.
+// 2.4 % longer than the best one on average, 19 % at worst.
 struct LinearTile { int bm, bn, resident; double block_us, tile_us, tflops; };
 constexpr LinearTile kLinearTiles[] = {
     {32, 128, 4, 0.43, 3.4, 434}, {32, 256, 2, 0.96, 3.3, 366}, {64, 128, 3, 0.57, 3.8, 500},
@@ -593,9 +669,9 @@ static int launch_linear(LinearParams &p, LinearPlan plan, void *workspace, void
     // (rows at odd addresses cost linear_rows_kernel more than they cost a tile: 1 x 50256 x 1023 48 us and in tiles 34)
     if (plan.tile < 0 && !direct && (int64_t)p.n * p.k > (1 << 24)) plan = {0, 1};
     if (plan.tile < 0) return launch(linear_rows_kernel<T>, dim3((unsigned)(((int64_t)p.n + 15) / 16)), kGroupThreads, p, stream, what);
-    // A tile's rows are addressed by 32-bit offsets, and every load is of eight columns: rows that lie further apart or are shorter
+    // A tile's rows are addressed by 32-bit offsets (of out and the residual the eight that a wavefront writes at a time), and every load is of eight columns: rows that lie further apart or are shorter
     // take the simple kernel.
-    const bool far = p.x_stride >= (1 << 21) || p.w_stride >= (1 << 21) || p.k < 8;
+    const bool far = p.x_stride >= (1 << 21) || p.w_stride >= (1 << 21) || p.out_stride >= (1 << 25) || p.residual_stride >= (1 << 25) || p.k < 8;
     const int64_t bm = far ? 64 : kLinearTiles[plan.tile].bm, bn = far ? 64 : kLinearTiles[plan.tile].bn;
     p.splits = far ? 1 : plan.splits;
     const int64_t grid = tile_grid((p.m + bm - 1) / bm, (p.n + bn - 1) / bn, p.splits);
@@ -674,7 +750,7 @@ extern "C" int bpe_linear(const void *x, int64_t x_stride, const void *weight, i
     p.x_stride = m > 1 ? x_stride : 0; p.w_stride = n > 1 ? weight_stride : 0;        // (of one row the stride says nothing)
     p.m = (int32_t)m; p.n = (int32_t)n; p.k = (int32_t)k;
     p.bias = bias; p.bias_dtype = bias_dtype; p.activation = activation;
-    p.residual = residual; p.residual_stride = residual_stride;
-    p.out = out; p.out_stride = out_stride; p.out_dtype = out_dtype;
+    p.residual = residual; p.residual_stride = residual && m > 1 ? residual_stride : 0;
+    p.out = out; p.out_stride = m > 1 ? out_stride : 0; p.out_dtype = out_dtype;
     return dtype == BPE_BF16 ? launch_linear<Bf16>(p, plan, workspace, stream) : launch_linear<F16>(p, plan, workspace, stream);
 }

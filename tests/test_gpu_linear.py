@@ -265,3 +265,19 @@ def test_activations_over_their_range(B):
         want = _act(v, act)
         tol = 4e-6 * np.abs(want) + 2.0 ** -24 * np.abs(want) + (0.75e-7 + 2 * 2.0 ** -24) * np.abs(v)
         assert (np.abs(out.double().cpu().numpy() - want) <= tol).all(), act
+
+
+@pytest.mark.parametrize("which", ["out", "residual", "both"])
+def test_far_rows_of_the_result(B, which):
+    """Rows of out or of the residual 2^25 elements apart and more, of x and weight next to each other."""
+    import torch
+    m, n, k = 20, 600, 64
+    stride = (1 << 25) + 8
+    x, w = _rand(torch, 1, m, k, dtype=torch.bfloat16), _rand(torch, 2, n, k, dtype=torch.bfloat16)
+    whole = torch.empty((m - 1) * stride + 4096, dtype=torch.bfloat16, device="cuda")
+    near = _rand(torch, 3, m, n, dtype=torch.bfloat16)
+    far = torch.as_strided(whole, (m, n), (stride, 1), 0)
+    out = torch.as_strided(whole, (m, n), (stride, 1), 1024) if which != "residual" else torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+    far.copy_(near)
+    _call(B, torch, x, w, out, residual=near if which == "out" else far)
+    _check(out, x, w, None, near, "none", "bfloat16")
