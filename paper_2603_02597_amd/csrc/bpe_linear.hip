@@ -564,7 +564,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 163840 / lds_of_tile(BM, BN, XS
                 if constexpr (kAhead) {
 #pragma unroll
                     for (int u = 0; u < kBatch; ++u) res[u] = next[u];
-                    fetch(p, row + kRows, kStep, j, next);
+                    if (32 * a + r + kRows < BM / WM) fetch(p, row + kRows, kStep, j, next);
                 } else {
                     fetch(p, row, kStep, j, res);
                 }
