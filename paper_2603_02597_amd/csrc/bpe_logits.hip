@@ -73,19 +73,22 @@ __global__ void __launch_bounds__(kAdjustThreads) adjust_kernel(AdjustParams p) 
         auto note = [&](int v) {
             if (v >= first && v < last) atomicAdd(&count[v - first], 1u);
         };
-        int i = begin + 4 * tid;
-        for (; i <= end - 4 - 12 * kAdjustThreads; i += 16 * kAdjustThreads) {
+        // (places within the row's list are unsigned, so that they pass its end without a wrap however long all the lists are)
+        const int32_t *history = r.history + begin;
+        const uint32_t length = (uint32_t)(end - begin);
+        uint32_t i = 4 * tid;
+        for (; i + (12 * kAdjustThreads + 4) <= length; i += 16 * kAdjustThreads) {
             Int4Any v[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = *(const Int4Any *)(r.history + i + q * 4 * kAdjustThreads);
+            for (int q = 0; q < 4; ++q) v[q] = *(const Int4Any *)(history + i + q * 4 * kAdjustThreads);
 #pragma unroll
             for (int q = 0; q < 4; ++q) { note(v[q][0]); note(v[q][1]); note(v[q][2]); note(v[q][3]); }
         }
-        for (; i <= end - 4; i += 4 * kAdjustThreads) {
-            const Int4Any v = *(const Int4Any *)(r.history + i);
+        for (; i + 4 <= length; i += 4 * kAdjustThreads) {
+            const Int4Any v = *(const Int4Any *)(history + i);
             note(v[0]); note(v[1]); note(v[2]); note(v[3]);
         }
-        for (; i < end; ++i) note(r.history[i]);          // (one thread's: the last one to three)
+        for (; i < length; ++i) note(history[i]);          // (one thread's: the last one to three)
         for (int i = bias_begin + tid; i < bias_end; i += kAdjustThreads) {
             const int v = r.bias_ids[i];
             if (v >= first && v < last) atomicOr(&count[v - first], kBiased);

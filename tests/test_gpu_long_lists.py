@@ -1,0 +1,34 @@
+"""bpe_adjust_logits where the list of all rows is as long as it may be: the places of the last rows' entries lie just
+below 2^31, and a workgroup's steps past a list's end pass it."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+MOST = (1 << 31) - 2                 # entries of a list
+KNOWN = 30000                        # of them at the end that are not the same everywhere
+VOCAB = 50
+
+
+@pytest.fixture(scope="module")
+def B():
+    import paper_2603_02597_amd as B
+    return B
+
+
+# places that rows begin and end at, counted from the end of the list
+@pytest.mark.parametrize("back", [[20000, 0], [16387, 3, 0, 0], [4096, 1, 0], [4100, 4, 0, 0, 0], [16400, 16384, 12289, 4099, 700, 5, 4, 3, 1, 0], [700, 690], [MOST, 0]], ids=str)
+def test_history_up_to_the_last_place(B, back):
+    import torch
+    print(f"[case] long history {back}", flush=True)
+    tail = np.random.default_rng(1).integers(-2, VOCAB + 2, KNOWN).astype(np.int32)
+    history = torch.full((MOST,), -1, dtype=torch.int32, device="cuda")
+    history[MOST - KNOWN:] = torch.from_numpy(tail).cuda()
+    rows = len(back) - 1
+    offsets = torch.tensor([MOST - b for b in back], dtype=torch.int32, device="cuda")
+    got = torch.empty(rows, VOCAB, device="cuda")
+    B.bpe_adjust_logits(torch.zeros(rows, VOCAB, device="cuda"), got, history=history, history_offsets=offsets, frequency=torch.ones(rows, device="cuda"))
+    want = np.zeros((rows, VOCAB))
+    for r in range(rows):
+        part = tail[max(KNOWN - back[r], 0):KNOWN - back[r + 1]]
+        want[r] -= np.bincount(part[(part >= 0) & (part < VOCAB)], minlength=VOCAB)
+    assert np.array_equal(got.cpu().numpy(), want)
