@@ -89,8 +89,8 @@ __global__ void __launch_bounds__(kAdjustThreads) adjust_kernel(AdjustParams p) 
             note(v[0]); note(v[1]); note(v[2]); note(v[3]);
         }
         for (; i < length; ++i) note(history[i]);          // (one thread's: the last one to three)
-        for (int i = bias_begin + tid; i < bias_end; i += kAdjustThreads) {
-            const int v = r.bias_ids[i];
+        for (uint32_t i = tid; i < (uint32_t)(bias_end - bias_begin); i += kAdjustThreads) {
+            const int v = r.bias_ids[(int64_t)bias_begin + i];
             if (v >= first && v < last) atomicOr(&count[v - first], kBiased);
         }
         __syncthreads();

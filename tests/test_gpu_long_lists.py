@@ -32,3 +32,27 @@ def test_history_up_to_the_last_place(B, back):
         part = tail[max(KNOWN - back[r], 0):KNOWN - back[r + 1]]
         want[r] -= np.bincount(part[(part >= 0) & (part < VOCAB)], minlength=VOCAB)
     assert np.array_equal(got.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("back", [[3000, 0], [1025, 1, 0, 0], [1024, 0, 0], [5, 0], [30000, 29000, 1023, 0]], ids=str)
+def test_biases_up_to_the_last_place(B, back):
+    """Of a token that a row lists more than once the last entry counts."""
+    import torch
+    print(f"[case] long bias lists {back}", flush=True)
+    rng = np.random.default_rng(2)
+    tail, tail_values = rng.integers(-2, VOCAB + 2, KNOWN).astype(np.int32), rng.integers(-9, 9, KNOWN).astype(np.float32)
+    ids = torch.full((MOST,), -1, dtype=torch.int32, device="cuda")
+    values = torch.full((MOST,), float("nan"), device="cuda")
+    ids[MOST - KNOWN:] = torch.from_numpy(tail).cuda()
+    values[MOST - KNOWN:] = torch.from_numpy(tail_values).cuda()
+    rows = len(back) - 1
+    offsets = torch.tensor([MOST - b for b in back], dtype=torch.int32, device="cuda")
+    got = torch.empty(rows, VOCAB, device="cuda")
+    B.bpe_adjust_logits(torch.ones(rows, VOCAB, device="cuda"), got, bias_ids=ids, bias_values=values, bias_offsets=offsets)
+    want = np.ones((rows, VOCAB))
+    for r in range(rows):
+        last = {int(v): x for v, x in zip(tail[KNOWN - back[r]:KNOWN - back[r + 1]], tail_values[KNOWN - back[r]:KNOWN - back[r + 1]])}
+        for v, x in last.items():
+            if 0 <= v < VOCAB:
+                want[r, v] += x
+    assert np.array_equal(got.cpu().numpy(), want)
