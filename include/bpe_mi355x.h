@@ -583,10 +583,10 @@ typedef struct {
     const float *bias_values;       /* [n_bias] */
     const int32_t *bias_offsets;    /* [rows + 1], clamped to [0, n_bias] */
     int64_t n_bias;                 /* < 2^31 */
-    const uint32_t *masks;          /* [n_masks] rows as bpe_grammar_masks writes them, mask_stride words apart */
+    const uint32_t *masks;          /* [n_masks] rows as bpe_grammar_masks writes them, mask_stride words apart; NULL: no row has a mask (of a table of 0 rows the address is any other) */
     int64_t mask_stride;
     int64_t n_masks;
-    const int32_t *mask_index;      /* [rows]: the row's mask, a negative value for none; one that is too large allows no token.  NULL: row r has mask r (n_masks >= rows) */
+    const int32_t *mask_index;      /* [rows]: the row's mask, a negative value for none; one that is too large allows no token.  Not without masks (BPE_ERR_NULL).  NULL: row r has mask r (n_masks >= rows) */
 } bpe_logit_rules;
 
 /*

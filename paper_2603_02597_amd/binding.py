@@ -706,6 +706,7 @@ def bpe_adjust_logits(logits, out, history=None, history_offsets=None, repetitio
         raise ValueError("bias_values and bias_offsets need bias_ids")
     if masks is not None:
         p_masks, s_masks = _mask_rows(masks, n_vocab)
+        p_masks = p_masks or po                    # (a tensor of no rows has no address, but is a table: any index is too large for it)
         n_masks = masks.shape[0]
         if mask_index is not None:
             p_index = _row_list(mask_index, "int32", rows, "mask_index")

@@ -621,6 +621,7 @@ extern "C" int bpe_adjust_logits(const void *logits, int64_t logits_stride, int 
         }
         if ((!r.history && r.n_history) || (!r.history != !r.history_offsets && r.n_history)) { set_error("bpe_adjust_logits: history and history_offsets come together"); return BPE_ERR_NULL; }
         if (r.n_bias && (!r.bias_ids || !r.bias_values || !r.bias_offsets)) { set_error("bpe_adjust_logits: bias_ids, bias_values and bias_offsets come together"); return BPE_ERR_NULL; }
+        if (!r.masks && r.mask_index) { set_error("bpe_adjust_logits: mask_index without masks"); return BPE_ERR_NULL; }
         if (r.masks && (r.n_masks > 1 && r.mask_stride < (n_vocab + 31) / 32)) { set_error("bpe_adjust_logits: mask_stride is shorter than a row"); return BPE_ERR_SIZE; }
         if (r.masks && !r.mask_index && r.n_masks < rows) { set_error("bpe_adjust_logits: without mask_index there is a mask for every row"); return BPE_ERR_SIZE; }
         p.rules = r;
