@@ -668,7 +668,20 @@ static int launch_linear(LinearParams &p, LinearPlan plan, void *workspace, void
     const bool direct = p.x_stride % 8 == 0 && p.w_stride % 8 == 0 && !(((uintptr_t)p.x | (uintptr_t)p.w) & 15);
     // (rows at odd addresses cost linear_rows_kernel more than they cost a tile: 1 x 50256 x 1023 48 us and in tiles 34)
     if (plan.tile < 0 && !direct && (int64_t)p.n * p.k > (1 << 24)) plan = {0, 1};
-    if (plan.tile < 0) return launch(linear_rows_kernel<T>, dim3((unsigned)(((int64_t)p.n + 15) / 16)), kGroupThreads, p, stream, what);
+    if (plan.tile < 0) {
+        constexpr int64_t kAtOnce = 16 * (kMaxThreads / kGroupThreads - 1);           // columns of a launch
+        for (int64_t done = 0; done < p.n; done += kAtOnce) {
+            LinearParams run = p;
+            run.n = (int32_t)std::min(p.n - done, kAtOnce);
+            run.w = p.w + done * p.w_stride;
+            run.out = (char *)p.out + done * dtype_bytes(p.out_dtype);
+            if (p.bias) run.bias = (const char *)p.bias + done * dtype_bytes(p.bias_dtype);
+            if (p.residual) run.residual = (const char *)p.residual + done * dtype_bytes(p.out_dtype);
+            const int rc = launch(linear_rows_kernel<T>, dim3((unsigned)(((int64_t)run.n + 15) / 16)), kGroupThreads, run, stream, what);
+            if (rc != BPE_OK) return rc;
+        }
+        return BPE_OK;
+    }
     // A tile's rows are addressed by 32-bit offsets (of out and the residual the eight that a wavefront writes at a time), and every load is of eight columns: rows that lie further apart or are shorter
     // take the simple kernel.
     const bool far = p.x_stride >= (1 << 21) || p.w_stride >= (1 << 21) || p.out_stride >= (1 << 25) || p.residual_stride >= (1 << 25) || p.k < 8;
