@@ -522,10 +522,10 @@ int64_t bpe_linear_workspace_bytes(int64_t m, int64_t n, int64_t k);
  *   out        device [m][n] of out_dtype (BPE_F32 or `dtype`)
  *   workspace  device, 256-byte aligned, >= bpe_linear_workspace_bytes(m, n, k); may be NULL if that is 0.
  *              Need not be initialised; calls that share one must be ordered on one stream
- * Products and sums in 32 bits, rounded once to out_dtype; gelu's erf is good to 1.5e-7, the other activations to the rounding of
- * 32 bits, and all give their limit at both infinities.  m, n, k >= 0, each below 2^30 (with k == 0 the sum is 0); matrices may have
- * more than 2^32 elements.  (BPE_ERR_SIZE too where out would take 2^24 workgroups, of 4,096 elements and more.)  The order of the
- * sum goes by the sizes, the strides and the alignment alone.
+ * Products and sums in 32 bits, rounded once to out_dtype.  The activations are good to so many 2^-24 of their value (or to 2^-119): gelu
+ * 20 + 2 v^2, silu 6 + 6 |v|, gelu by tanh 6 + 6 x with x = twice the argument of tanh; all give their limit at both infinities.
+ * m, n, k >= 0, each below 2^30 (with k == 0 the sum is 0); matrices may have more than 2^32 elements.  (BPE_ERR_SIZE too where out
+ * would take 2^24 workgroups, of 4,096 elements and more.)  The order of the sum goes by the sizes, the strides and the alignment alone.
  */
 int bpe_linear(const void *x, int64_t x_stride, const void *weight, int64_t weight_stride, int dtype,
                int64_t m, int64_t n, int64_t k, const void *bias, int bias_dtype, const void *residual,

@@ -43,11 +43,14 @@ __device__ __forceinline__ float relu(float v) { return v < 0.0f ? 0.0f : v; }
 __device__ __forceinline__ float times_sigmoid(float v, float minus_log2_odds) {
     return fmaxf(v, -kMost) * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(minus_log2_odds));
 }
-// v (1 + erf(v / sqrt 2)) / 2 = max(v, 0) - |v| q with q = (1 - erf(|v| / sqrt 2)) / 2, by the approximation 7.1.26 of Abramowitz and
-// Stegun's handbook, which is good to 1.5e-7 of 1 (its coefficients by 1 / 2, its p by 1 / sqrt 2).
+// v (1 + erf(v / sqrt 2)) / 2 = max(v, 0) - |v| q with q = erfc(|v| / sqrt 2) / 2, which is exp(-v^2 / 2) by a function that falls slowly: a
+// series of eight terms in t = 1 / (1 + 0.3 |v|), fitted to a relative error of 2.2e-7 (3.3e-9 of |v|) for |v| up to 14, where q leaves
+// 32 bits.  No difference of nearly equal numbers, so small results are good too: rms error 2.1e-8 on normal v, 1.6e-9 on -6 .. -2 (0.5 v (1
+// + erff(v / sqrt 2)): 2.5e-8, 3.4e-8; 2000 x 20000 x 512 f16 107 us, without an activation 76).
 __device__ __forceinline__ float gelu(float v) {
-    const float size = __builtin_fabsf(v), t = __builtin_amdgcn_rcpf(1.0f + (0.3275911f * 0.70710678118654752f) * size);
-    const float series = t * (0.127414796f + t * (-0.142248368f + t * (0.7107068705f + t * (-0.7265760135f + t * 0.5307027145f))));
+    const float size = __builtin_fabsf(v), t = __builtin_amdgcn_rcpf(1.0f + 0.3f * size);
+    const float series = t * (0.11962141f + t * (0.120887813f + t * (0.0989954205f + t * (0.13186087f + t * (-0.0604071882f + t * (0.214153407f +
+                         t * (-0.161994644f + t * 0.0368829476f)))))));
     return fmaxf(v, 0.0f) - fminf(size, kMost) * (series * __builtin_amdgcn_exp2f(v * v * (-0.5f * kLog2Of)));
 }
 // v (1 + tanh u) / 2 = v / (1 + exp(-2 u)), u = sqrt(2 / pi) (v + 0.044715 v^3)
