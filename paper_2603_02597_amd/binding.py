@@ -612,7 +612,15 @@ class Grammar:
 
     def __init__(self, transitions, accepting=None):
         lib = load_library()
-        t, tp = _host_i32(transitions, (-1, 256))
+        t = np.asarray(transitions)
+        if t.ndim == 2 and t.shape[1] != 256:
+            raise ValueError(f"transitions: expected 256 columns, one per byte, got {t.shape[1]}")
+        if t.dtype.kind not in "iub":
+            t = t.astype(np.float64)
+            if not (t == np.floor(t)).all():
+                raise ValueError("transitions: expected whole numbers")
+        # (every negative value ends a walk and none from n_states on is a state, in whatever width they come)
+        t, tp = _host_i32(np.clip(t, -1, 2**31 - 1), (-1, 256))
         a = None if accepting is None else np.ascontiguousarray(np.asarray(accepting) != 0, dtype=np.uint8).reshape(-1)
         if a is not None and a.size != t.shape[0]:
             raise ValueError(f"accepting has {a.size} entries for {t.shape[0]} states")
