@@ -97,12 +97,17 @@ __global__ void __launch_bounds__(kGroupThreads) grammar_masks_kernel(MaskParams
 // one state after the other.  Most states let few bytes pass: one look at the transitions per class says which, and only the
 // tokens behind those are walked, which the tile holds in order of their first class.  Where many tokens pass, all are walked
 // in order of their ids, four per lane at a time, so that four chains of reads are under way together.  1,500 states of 50,257 tokens:
-// 45 us, of which 17 lay out the tiles; bound by instructions (the bytes are 9.4 MB of masks, 2 us), with transitions in LDS.
+// 45 us, of which 17 lay out the tiles; bound by instructions (the bytes are 9.4 MB of masks, 2 us), with transitions in LDS.  Long tokens
+// are walked by a lane each while the others wait: 1,500 states of 100,256 tokens, of up to 2,049 bytes, 2.8 ms.
 constexpr int kMaskTile = 2048, kMaskThreads = 1024, kMaskWaves = kMaskThreads / kWave;
 static_assert(kMaskTile == 32 * kWave, "a word of bits per lane");
 constexpr int kMaskTable = 48 * 1024;            // transitions that are kept in LDS
 constexpr int kMaskStates = 2048;                // states of a workgroup that are at hand at a time
-constexpr int kMaskFew = 5;                      // behind up to so many classes tokens are walked class by class
+// Behind up to so many classes tokens are walked class by class.  1,500 states of 50,257 tokens, as many letters lead on from each: 1 letter 17 us
+// class by class and 97 all tokens, 3 letters 24 and 96, 5 letters 33 and 100, 8 letters 47 and 112, 12 letters 70 and 138, all 26 the
+// same 116; a grammar of words and free text 42, with all of it class by class 74.  (So 5 is on the safe side for letters, more so for bytes
+// that few tokens begin with; what counts is how many tokens those are, not how many classes.)
+constexpr int kMaskFew = 5;
 template <bool IN_LDS>
 __global__ void __launch_bounds__(kMaskThreads) grammar_tile_masks_kernel(MaskParams p) {
     __shared__ uint32_t start[257], filled[256];

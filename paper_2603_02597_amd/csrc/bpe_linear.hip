@@ -308,11 +308,11 @@ __global__ void __launch_bounds__(kGroupThreads) linear_rows_kernel(LinearParams
 // linear_join_kernel adds up where there are fewer tiles than compute units (plan_linear).
 // The loads go straight into LDS, two blocks ahead; products, LDS reads and loads are put in order by hand, so the matrix cores
 // see no wait but the one in the middle of a block.  The operands are swapped (weight on the left): a lane ends with neighbouring
-// columns of a row.  Bound by memory for few rows: 64 x 100256 x 4096 155 us, 5.4 TB/s.  Bound by the matrix cores for many: 4001 x
-// 50256 x 4096 1,356 us, 1,215 TFLOP/s, 95 % of a library's plain product there; 4096 x 4096 x 4096 119 us, 87 %.  What is missing is a
+// columns of a row.  Bound by memory for few rows: 64 x 100256 x 4096 163 us, 5.2 TB/s.  Bound by the matrix cores for many: 4001 x
+// 50256 x 4096 1,301 to 1,395 us by card, 1,266 to 1,181 TFLOP/s, 94 % of a library's plain product there; 4096 x 4096 x 4096 119 us, 87 %.  What is missing is a
 // tile's first loads and its result, some 10 us in which the only workgroup of a compute unit leaves the matrix cores alone.
-// A last block that is cut off costs about a whole one: 120 x 3664 x 2792 17.0 us, x 2816 15.2.  Rows at odd addresses pass through
-// registers: 508 x 2086 x 579 13.6 us, 508 x 2088 x 584 10.
+// A last block that is cut off costs about a whole one: 120 x 3664 x 2792 16.2 us, x 2816 14.9.  Rows at odd addresses pass through
+// registers: 508 x 2086 x 579 13.1 us, 508 x 2088 x 584 10.2; 64 x 100256 x 4096 231 us, 4001 x 20000 x 2048 383, aligned 163 and 294.
 typedef float F16v __attribute__((ext_vector_type(16)));
 // D = A B + C on 32 x 32 x 16: lane l gives A[l % 32][8 (l / 32) ..+7] and B[8 (l / 32) ..+7][l % 32] and holds
 // C[e % 4 + 8 (e / 4) + 4 (l / 32)][l % 32] in element e.
@@ -628,8 +628,9 @@ __global__ void __launch_bounds__(kGroupThreads) linear_join_kernel(LinearParams
 // Which tiles a product of these sizes takes, and into how many parts k is cut: what an estimate of the time says.  A tile's
 // row: its sides, how many of its workgroups a compute unit holds, us for a block of 64 columns when a workgroup waits for
 // its loads alone, us for its first loads and its result, and the TFLOP/s of the whole chip when nothing else bounds it.  The
-// numbers are fitted to the times of all tiles and parts on 93 sizes (m 5 to 8192, n 256 to 128000, k 64 to 4096); there the choice takes
-// 2.4 % longer than the best one on average, 19 % at worst.
+// numbers are fitted to the times of all tiles and parts on 93 sizes (m 5 to 8192, n 256 to 128000, k 64 to 4096) as these were before whole
+// tiles left by uniform addresses; as they are now, the choice takes 2.4 % longer there than the best one on average, 19 % at worst.  (They are numbers that choose well;
+// not every one is a property of its tile.)
 struct LinearTile { int bm, bn, resident; double block_us, tile_us, tflops; };
 constexpr LinearTile kLinearTiles[] = {
     {32, 128, 4, 0.43, 3.4, 434}, {32, 256, 2, 0.96, 3.3, 366}, {64, 128, 3, 0.57, 3.8, 500},
@@ -669,7 +670,8 @@ static int launch_linear(LinearParams &p, LinearPlan plan, void *workspace, void
     const char *what = "bpe_linear launch";
     p.splits = 1;
     const bool direct = p.x_stride % 8 == 0 && p.w_stride % 8 == 0 && !(((uintptr_t)p.x | (uintptr_t)p.w) & 15);
-    // (rows at odd addresses cost linear_rows_kernel more than they cost a tile: 1 x 50256 x 1023 48 us and in tiles 34)
+    // (rows at odd addresses cost linear_rows_kernel more than they cost a tile: 1 x 50256 x 1023 46 us and in tiles 27, 4 x 100256 x
+    // 4096 448 and 209; 1 x 20000 x 1023 20 and 21)
     if (plan.tile < 0 && !direct && (int64_t)p.n * p.k > (1 << 24)) plan = {0, 1};
     if (plan.tile < 0) {
         constexpr int64_t kAtOnce = 16 * (kMaxThreads / kGroupThreads - 1);           // columns of a launch
