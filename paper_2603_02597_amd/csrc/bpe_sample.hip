@@ -83,7 +83,13 @@ struct Weights {
 struct Bins {
     float scale;
     __device__ __forceinline__ explicit Bins(double slope) : scale((float)fmin(kBinsPerOctave * slope, 1e30)) {}
-    __device__ __forceinline__ int operator()(float x) const { return (int)__builtin_floorf(fminf(fmaxf(x * scale, -1e9f), 1e9f)); }
+    // A logit's place among the bins, rounded by itself: fused with a sum behind it, a product just below a whole number would not be what it is where
+    // the bins are counted.
+    __device__ __forceinline__ float place(float x) const {
+#pragma clang fp contract(off)
+        return x * scale;
+    }
+    __device__ __forceinline__ int operator()(float x) const { return (int)__builtin_floorf(fminf(fmaxf(place(x), -1e9f), 1e9f)); }
 };
 
 // What a row's request asks for.
@@ -673,8 +679,8 @@ template <class T, bool FILTERS> struct SampleRow {
             __syncthreads();
             if (tid == 0) { list.in_list = 0; list.in_sifted = 0; list.least_key = ~0u; list.most_key = 0; }
             __syncthreads();
-            // Bins are the whole parts of x * scale, so the same comparison does without rounding down.  First sixteen bytes at a time: those that
-            // hold anything within half the width of the middle are kept; then those one by one.  (Atomics on one address go one after the
+            // Bins are the whole parts of bin.place, so comparing that does without rounding down.  First sixteen bytes at a time: those that hold
+            // anything within half the width of the middle (multiples of 1/2 below 2^23: the difference may be rounded to half, not past it) are kept; then those one by one.  (Atomics on one address go one after the
             // other: a wavefront reserves its places at once.)
             const float low = (float)(top - to), high = (float)(top - from + 1), middle = 0.5f * (low + high), half = 0.5f * (high - low);
             const auto look = [&](U4 raw, int c) {
@@ -682,7 +688,7 @@ template <class T, bool FILTERS> struct SampleRow {
                 __builtin_memcpy(some, &raw, 16);
                 float near = INFINITY;
 #pragma unroll
-                for (int e = 0; e < kPer; ++e) near = fminf(near, __builtin_fabsf(to_float<T>(some[e]) * bin.scale - middle));
+                for (int e = 0; e < kPer; ++e) near = fminf(near, __builtin_fabsf(bin.place(to_float<T>(some[e])) - middle));
                 const U64 found = __ballot(near <= half);
                 if (!found) return;
                 uint32_t at = 0;
@@ -720,7 +726,7 @@ template <class T, bool FILTERS> struct SampleRow {
                 uint32_t in_bins = 0;
 #pragma unroll
                 for (int e = 0; e < kPer; ++e) {
-                    const float scaled = to_float<T>(some[e]) * bin.scale;
+                    const float scaled = bin.place(to_float<T>(some[e]));
                     // (the row's last sixteen bytes may hold logits that other ones hold too)
                     in_bins |= (uint32_t)(scaled >= low && scaled < high && token + e >= first_at) << e;
                 }
