@@ -72,7 +72,8 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, CHUNKS > 1 ? 4 
         for (int u = 0; u < CHUNKS; ++u) load8(p.residual, row * p.residual_stride, 8 * (tid + u * THREADS), p.width, p.total_dtype, h[u]);
     }
     int turn = 0;
-    // what every element is moved and multiplied by
+    // what every element is moved and multiplied by (of the columns that exist: behind a row's end a first norm without a weight leaves what it makes of 0)
+    const auto exists = [&](int u, int e) { return 8 * (tid + u * THREADS) + e < p.width; };
     auto statistics = [&](int kind, float eps, float &mean, float &factor) {
         mean = 0;
         if (kind == BPE_NORM_LAYER) {
@@ -80,7 +81,7 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, CHUNKS > 1 ? 4 
 #pragma unroll
             for (int u = 0; u < CHUNKS; ++u)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum += v[u][e];
+                for (int e = 0; e < 8; ++e) sum += exists(u, e) ? v[u][e] : 0.0f;
             mean = row_sum<THREADS>(sum, lds, turn) * over;
             turn ^= 1;
         }
@@ -89,7 +90,7 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, CHUNKS > 1 ? 4 
         for (int u = 0; u < CHUNKS; ++u)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float d = 8 * (tid + u * THREADS) + e < p.width ? v[u][e] - mean : 0.0f;
+                const float d = exists(u, e) ? v[u][e] - mean : 0.0f;
                 squares = __builtin_fmaf(d, d, squares);
             }
         factor = 1.0f / __builtin_sqrtf(row_sum<THREADS>(squares, lds, turn) * over + eps);
