@@ -678,7 +678,8 @@ int64_t bpe_linear_mx_workspace_bytes(int64_t m, int64_t n, int64_t k, int x_dty
  *   weight  a 4-bit matrix of n rows and k columns
  *   out     device [m][n] of out_dtype: BPE_F32 or x_dtype, any of the three types for x in 4 bits
  * and everything else as for bpe_linear (but for the workgroups' parts of out: 1,024 elements and more).  Products are exact and summed in 32
- * bits, of which sums below 2^-126 may leave nothing.
+ * bits, of which sums below 2^-126 may leave nothing.  For x in 16 bits weights of 2^128 and more are infinities, as bpe_mx_rows gives them; x in 4
+ * bits takes them as they are.
  */
 int bpe_linear_mx(const void *x, int64_t x_stride, int x_dtype, const void *weight, int64_t m, int64_t n, int64_t k, const void *bias,
                    int bias_dtype, const void *residual, int64_t residual_stride, int activation, void *out, int64_t out_stride,

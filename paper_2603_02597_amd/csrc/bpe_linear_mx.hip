@@ -25,19 +25,29 @@ template <int S> __device__ __forceinline__ F16v mma_mx4(U4 a, U4 b, F16v c, uin
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, S, (int)scale_a, S, (int)scale_b);
 }
 
-// Two elements of f16 as two bf16 parts each, which hold all 11 bits: no scale of a weight leaves the range of bf16, as it would that of f16.
+// Two elements of f16 as two bf16 parts each, which hold all 11 bits: no scale of a weight leaves the range of bf16, as it would that of f16.  The first part
+// is the element cut off behind 8 bits, so the second has its sign or is 0; of an infinity the first is f16's largest number, cut off, and the second the infinity.
 __device__ __forceinline__ void split_f16(uint32_t two, uint32_t &high, uint32_t &low) {
+    constexpr float kMostF16 = 65504.0f;
     const float a = to_float<F16>((uint16_t)two), b = to_float<F16>((uint16_t)(two >> 16));
-    const uint16_t ha = from_float<Bf16>(a), hb = from_float<Bf16>(b);
-    // (an infinity has no second part: inf - inf would make it NaN)
-    const float la = __builtin_fabsf(a) < INFINITY ? a - to_float<Bf16>(ha) : 0.0f, lb = __builtin_fabsf(b) < INFINITY ? b - to_float<Bf16>(hb) : 0.0f;
-    high = (uint32_t)ha | (uint32_t)hb << 16;
-    low = (uint32_t)from_float<Bf16>(la) | (uint32_t)from_float<Bf16>(lb) << 16;
+    const uint32_t ha = __builtin_bit_cast(uint32_t, __builtin_amdgcn_fmed3f(a, -kMostF16, kMostF16)) & 0xffff0000u;
+    const uint32_t hb = __builtin_bit_cast(uint32_t, __builtin_amdgcn_fmed3f(b, -kMostF16, kMostF16)) & 0xffff0000u;
+    const uint32_t la = __builtin_bit_cast(uint32_t, a - __builtin_bit_cast(float, ha)), lb = __builtin_bit_cast(uint32_t, b - __builtin_bit_cast(float, hb));
+    high = __builtin_amdgcn_perm(hb, ha, 0x07060302);
+    low = __builtin_amdgcn_perm(lb, la, 0x07060302);
 }
-// Eight elements of x times as many of weight; `low`: the second parts of f16.
-template <class T, bool X_LEFT = false> __device__ __forceinline__ F16v mma_by_weight(U4 w, U4 x, U4 low, F16v c) {
+// Weights for the second parts: the largest number in the place of an infinity (a weight of 2^128 and more), whose product with a part of 0 would be NaN.  The
+// product with the first part is the infinity, and this one's has the same sign.  (NaN becomes a number: the first product has it.)
+__device__ __forceinline__ U4 finite_of(U4 w) {
+    typedef int16_t S8 __attribute__((ext_vector_type(8)));
+    const H8 negative = __builtin_elementwise_min(__builtin_bit_cast(H8, w), (H8)0xff7f);
+    return __builtin_bit_cast(U4, __builtin_elementwise_min(__builtin_bit_cast(S8, negative), (S8)0x7f7f));
+}
+constexpr float kMayBeInfinite = 0x1p126f;             // the least scale by which a code is 2^128 and more
+// Eight elements of x times as many of weight; of f16 the second parts `low` by finite weights.
+template <class T, bool X_LEFT = false> __device__ __forceinline__ F16v mma_by_weight(U4 w, U4 finite, U4 x, U4 low, F16v c) {
     c = X_LEFT ? mma32<Bf16>(x, w, c) : mma32<Bf16>(w, x, c);
-    if constexpr (T::kCode == BPE_F16) c = X_LEFT ? mma32<Bf16>(low, w, c) : mma32<Bf16>(w, low, c);
+    if constexpr (T::kCode == BPE_F16) c = X_LEFT ? mma32<Bf16>(low, finite, c) : mma32<Bf16>(finite, low, c);
     return c;
 }
 template <class T> __device__ __forceinline__ F16v mma_by_weight(U4 w, U4 x, F16v c) {
@@ -53,7 +63,7 @@ template <class T> __device__ __forceinline__ F16v mma_by_weight(U4 w, U4 x, F16
         }
         x = high;
     }
-    return mma_by_weight<T>(w, x, low, c);
+    return mma_by_weight<T>(w, finite_of(w), x, low, c);
 }
 
 // Products whose result leaves by put_wide take column 4 j + b of a wavefront's 128 in lane j of product b.  Of a group of 32 rows in LDS every
@@ -299,9 +309,13 @@ __global__ void __launch_bounds__(WM *WN *kWave, BM * BN > 32768 ? 1 : 2) linear
         if (q < TN) codes[into][b] = *(const U4 *)(lds + slot + (kWide ? wide_group * 1024 + wide_place(lane, b) : (wn * TN + b) * 1024 + 16 * lane));
         else scale[into][b] = scale_of(*(const uint8_t *)(lds + kScales + (t >> 2 & 1) * kS + (kWide ? wide_group * 256 + wide_scale(lane, b) : (wn * TN + b) * 256 + 4 * lane) + (t & 3)));
     };
-    U4 wf[2][TN];                      // of a step, and of the next one
+    constexpr bool kParts = T::kCode == BPE_F16;
+    U4 wf[2][TN], finite[2][TN];       // of a step, and of the next one; for the second parts of f16
     U4 high[2], low[2];                // the parts of a fragment of x in f16, and of the next one
-    const auto widen = [&](int from, int step, int into, int b) { wf[into][b] = bf16_of(codes[from][b][step], scale[from][b]); };
+    const auto widen = [&](int from, int step, int into, int b) {
+        wf[into][b] = bf16_of(codes[from][b][step], scale[from][b]);
+        if constexpr (kParts) finite[into][b] = finite_of(wf[into][b]);
+    };
     constexpr int kReadsX = 2 * TM, kProducts = 2 * TM * TN;
     // The products of one half of block t.  Among them: the reads of x of the other half (of the block in slot xr), in the second half codes and scales of the
     // next block, the weights of the next step, and loads.
@@ -328,9 +342,8 @@ __global__ void __launch_bounds__(WM *WN *kWave, BM * BN > 32768 ? 1 : 2) linear
                 for (int l = q * kLoadsX / kProducts; l < (q + 1) * kLoadsX / kProducts; ++l) store_x(xs, l);
             }
             // (of f16 the parts of the next fragment of x are made meanwhile)
-            constexpr bool kParts = T::kCode == BPE_F16;
             const int now = (2 * half + s) * TM + a & 1;
-            acc[a][b] = mma_by_weight<T, kWide>(wf[s][b], kParts ? high[now] : xf[half][s][a], low[now], acc[a][b]);
+            acc[a][b] = mma_by_weight<T, kWide>(wf[s][b], finite[s][b], kParts ? high[now] : xf[half][s][a], low[now], acc[a][b]);
             if constexpr (kParts) {
                 const int next_a = a + 1 < TM ? a + 1 : 0, next_s = a + 1 < TM ? s : s + 1;
                 const U4 &next = next_s < 2 ? xf[half][next_s & 1][next_a] : xf[half ^ 1][0][next_a];
@@ -494,6 +507,7 @@ __global__ void __launch_bounds__(kGroupThreads, T::kCode == BPE_F16 && TM == 2 
                 }
                 *to = high;
                 to[kPart / 16] = low;
+                __builtin_amdgcn_sched_barrier(0);             // (not all parts at once: registers would spill)
             } else {
                 *to = xr[u];
             }
@@ -510,7 +524,7 @@ __global__ void __launch_bounds__(kGroupThreads, T::kCode == BPE_F16 && TM == 2 
         }
     };
     F16v acc[TM][TN] = {};
-    const auto products = [&](auto which) {
+    const auto products = [&](auto which, auto infinite) {
         constexpr int I = decltype(which)::value;
 #pragma unroll
         for (int s = 0; s < 4; ++s)
@@ -527,7 +541,7 @@ __global__ void __launch_bounds__(kGroupThreads, T::kCode == BPE_F16 && TM == 2 
                 for (int b = 0; b < TN; ++b) {
                     const U4 wide = bf16_of(codes[I][b][s][q], scale_of(scales[I][b] >> 8 * s & 255));
 #pragma unroll
-                    for (int a = 0; a < TM; ++a) acc[a][b] = mma_by_weight<T>(wide, x[a], low[a], acc[a][b]);
+                    for (int a = 0; a < TM; ++a) acc[a][b] = mma_by_weight<T>(wide, decltype(infinite)::value ? finite_of(wide) : wide, x[a], low[a], acc[a][b]);
                 }
             }
     };
@@ -539,7 +553,18 @@ __global__ void __launch_bounds__(kGroupThreads, T::kCode == BPE_F16 && TM == 2 
         const int ahead = min(panel + 1, end - 1);             // (behind the last panel: that one again, for nobody)
         load_x(ahead);
         load_w(next, ahead);
-        products(now);
+        // (weights that are infinities, which hardly any matrix has, have products of their own: finite_of for every weight takes 5 to 12 % longer)
+        bool infinite = false;
+        if constexpr (kParts) {
+            uint32_t most = 0;
+#pragma unroll
+            for (int b = 0; b < TN; ++b)
+#pragma unroll
+                for (int s = 0; s < 4; ++s) most = max(most, scales[decltype(now)::value][b] >> 8 * s & 255);
+            infinite = __any(scale_of(most) >= kMayBeInfinite);
+        }
+        if (infinite) products(now, std::true_type());
+        else products(now, std::false_type());
         store_x(decltype(next)::value);
     };
     if (panel < end) {
