@@ -524,7 +524,7 @@ __global__ void __launch_bounds__(kGroupThreads, T::kCode == BPE_F16 && TM == 2 
         }
     };
     F16v acc[TM][TN] = {};
-    const auto products = [&](auto which, auto infinite) {
+    const auto products = [&](auto which, auto infinite) __attribute__((always_inline)) {
         constexpr int I = decltype(which)::value;
 #pragma unroll
         for (int s = 0; s < 4; ++s)
@@ -563,7 +563,7 @@ __global__ void __launch_bounds__(kGroupThreads, T::kCode == BPE_F16 && TM == 2 
                 for (int s = 0; s < 4; ++s) most = max(most, scales[decltype(now)::value][b] >> 8 * s & 255);
             infinite = __any(scale_of(most) >= kMayBeInfinite);
         }
-        if (infinite) products(now, std::true_type());
+        if (__builtin_expect(infinite, false)) products(now, std::true_type());
         else products(now, std::false_type());
         store_x(decltype(next)::value);
     };
