@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 1) linear_mx4_block_kernel(Line
 // ..+7 of the 64 in product q, of x and weight alike, so that each of its sixteen bytes of weight has one scale.  x of block t + 2 is
 // loaded in the first half of block t, weight in the second; scales, of four blocks, with the first of them.
 // Bound by the matrix cores in 256 x 256 (2003 x 50256 x 4096 708 us, 1165 TFLOP/s, with silu and a residual 766); f16, whose two parts are two
-// products, takes twice as long (1457).  Rows of x at odd addresses pass through registers, which 256 x 256 has none left for: 1075 in 128 x 128.
+// products, takes twice as long (1,394 to 1,502 by card; bf16 664 to 708).  Rows of x at odd addresses pass through registers, which 256 x 256 has none left for: 1075 in 128 x 128.
 constexpr int kXSlots = 3;
 template <class T, class OUT, int BM, int BN, int WM, int WN, bool DIRECT>
 __global__ void __launch_bounds__(WM *WN *kWave, BM * BN > 32768 ? 1 : 2) linear_x16_block_kernel(LinearMx4Params p) {

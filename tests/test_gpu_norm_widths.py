@@ -38,3 +38,14 @@ def test_a_row_of_one_element(B, torch):  # noqa: F811
     assert torch.equal(total, 2 * h + 1) and (out == -0.75).all()
     B.bpe_norm(y, out, post="layer", residual=h, total=total, pre="layer")
     assert torch.equal(total, h) and (out == 0).all()
+
+
+def test_squares_beyond_32_bits(B, torch):  # noqa: F811
+    """A sum of squares that passes the largest float leaves the bias, and the total is what it is."""
+    y = torch.full((3, 300), 1e25, device="cuda")
+    y[1] = 2.0
+    b = torch.randn(300, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    total, out = torch.empty_like(y), torch.empty_like(y)
+    B.bpe_norm(y, out, total=total, pre="rms", pre_bias=b, eps=0.0)
+    assert torch.equal(total, y) and torch.equal(out[[0, 2]], b.expand(2, 300))
+    assert (out[1] - (1 + b)).abs().max() <= 4 * 2.0 ** -24 * (1 + b.abs().max())
